@@ -303,6 +303,55 @@ int hdt_cross_attn_bwd(const int8_t *level, const int32_t *cu_seqlens_k, const i
                        size_t workspace_bytes, void *stream);
 
 /*
+ * Dropout from a counter-based generator (the paper fine-tunes with dropout 0.1): y = residual + D o x, where D is
+ * 0 or the reciprocal of the probability of being kept.  D is a function of (seed, offset, site, row, column) and is
+ * never stored: the gradient with respect to x is the same call on d_y without a residual, the one with respect to
+ * the residual is d_y itself.
+ *   Eight columns of a row take one 128-bit block of Philox-4x32-10 (Salmon et al., SC 2011): key = the 64 bits of
+ *   seed, counter = (column / 8, row, site, low 32 bits of offset).  Column c keeps its value if the (c mod 8)-th
+ *   16-bit half word of the block (low half of a word first) is at least t = floor(65536 p + 1/2), t <= 65535, and is
+ *   then multiplied by 65536 / (65536 - t).
+ *   x, residual, y     device [rows, cols] of `dtype`, contiguous; residual may be NULL; y may be x or residual
+ *   rng                device int64 [2]: seed, offset.  In device memory, so that a captured graph draws a new mask
+ *                      at every replay once its caller has advanced the offset
+ *   site               tells the dropouts of one network apart that share a state
+ *   p                  in [0, 1)
+ * rows < 2^31 - 255, 1 <= cols <= 8192.  Rows whose length is a multiple of 8 in tensors that are 16-byte aligned are the fast
+ * case; any other alignment to the element works.  Arithmetic in fp32, rounded once.  Asynchronous on `stream`.
+ */
+int hdt_dropout(const void *x, const void *residual, const int64_t *rng, int32_t site, int64_t rows, int32_t cols,
+                int32_t dtype, float p, void *y, void *stream);
+
+/*
+ * Layer norm over the last dimension with the residual sum and the dropout in front of it: what lies between two
+ * sub-layers of a pre-norm block (paper, paragraph "Hierarchical Encoder and Decoder Stacks").
+ *     h = residual + D o x,   y = (h - mean) rstd weight + bias,   rstd = 1 / sqrt(var + eps)
+ * (var over the columns, not corrected; mean and rstd belong to h before it is rounded to `dtype`).  Backward, with
+ * xhat = (h - mean) rstd and g = d_y weight:
+ *     d_residual = rstd (g - mean(g) - xhat mean(g xhat)) + d_h,   d_x = D o d_residual,
+ *     d_weight = sum over rows of d_y xhat,   d_bias = sum over rows of d_y.
+ *   x, residual, h, y, d_y, d_h, d_residual, d_x   device [rows, cols] of `dtype`, contiguous
+ *   weight, bias, d_weight, d_bias                 device [cols] of w_dtype: HDT_F32, or `dtype`
+ *   mean, rstd         device float [rows], written by the forward, read by the backward
+ *   residual           NULL: none.  d_h, the gradient that h gets from the residual stream, NULL: none
+ *   rng, site, p       as in hdt_dropout; p = 0: no dropout, rng may be NULL
+ *   h                  may be x or residual; may be NULL where it is x itself (no residual and p = 0)
+ *   d_x                written with p > 0 only (else it is d_residual); may be d_h, as may d_residual
+ *   workspace          device, >= hdt_layer_norm_workspace_bytes(rows, cols), 256-byte aligned: column sums of the
+ *                      kernel's blocks, added up in a fixed order (the same bits every run)
+ * Sizes and alignment as for hdt_dropout.  Without rows the backward writes zeros to d_weight and d_bias.
+ * Asynchronous on `stream`.
+ */
+int hdt_layer_norm_fwd(const void *x, const void *residual, const void *weight, const void *bias, const int64_t *rng,
+                       int32_t site, float p, int64_t rows, int32_t cols, int32_t dtype, int32_t w_dtype, float eps,
+                       void *h, void *y, float *mean, float *rstd, void *stream);
+size_t hdt_layer_norm_workspace_bytes(int64_t rows, int32_t cols);
+int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const float *mean, const float *rstd,
+                       const void *weight, const int64_t *rng, int32_t site, float p, int64_t rows, int32_t cols,
+                       int32_t dtype, int32_t w_dtype, void *d_residual, void *d_x, void *d_weight, void *d_bias,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Waits for `stream`, then returns and clears the first failure a kernel of this library
  * recorded on the device: HDT_ERR_TIMEOUT when a bounded wait (on a TMA or tensor-core
  * completion barrier) ran out; results of that call are then undefined.  HDT_OK if none.

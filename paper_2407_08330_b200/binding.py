@@ -79,6 +79,14 @@ def lib():
         L.hdt_cross_attn_bwd.restype = C.c_int
         L.hdt_cross_attn_bwd.argtypes = [C.c_void_p] * 3 + [C.c_int32] * 4 + [C.c_void_p] * 9 + [C.c_int32] * 3 + \
                                         [C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.hdt_dropout.restype = C.c_int
+        L.hdt_dropout.argtypes = [C.c_void_p] * 3 + [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p]
+        L.hdt_layer_norm_fwd.restype = C.c_int
+        L.hdt_layer_norm_fwd.argtypes = [C.c_void_p] * 5 + [C.c_int32, C.c_float, C.c_int64] + [C.c_int32] * 3 + [C.c_float] + [C.c_void_p] * 5
+        L.hdt_layer_norm_workspace_bytes.restype = C.c_size_t
+        L.hdt_layer_norm_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+        L.hdt_layer_norm_bwd.restype = C.c_int
+        L.hdt_layer_norm_bwd.argtypes = [C.c_void_p] * 7 + [C.c_int32, C.c_float, C.c_int64] + [C.c_int32] * 3 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
         L.hdt_set_option.restype = C.c_int
         L.hdt_device_status.restype = C.c_int
         L.hdt_device_status.argtypes = [C.c_void_p]
@@ -346,6 +354,113 @@ def hdt_cross_attn_bwd(level, cu_seqlens_k, cu_seqlens_q, level_mask, q, k, v, o
                                 k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), H, d,
                                 _DTYPES[q.dtype], float(softmax_scale), workspace.data_ptr(), workspace.numel(), _stream()))
     return dq, dk, dv
+
+
+def _here(*tensors):
+    """The tensors of a call are contiguous and on the current device, whose current stream the call goes to."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.device.index == dev and t.is_contiguous()):
+            raise HdtError(-1, "every tensor must be contiguous and on the current CUDA device")
+
+
+def _rng(rng, p):
+    if rng is None:
+        return None
+    if rng.dtype != torch.int64 or rng.numel() != 2:
+        raise HdtError(-1, "rng must be int64 [2]: seed, offset")
+    _here(rng)
+    return rng.data_ptr()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _like(t, *others):
+    for x in others:
+        if x is not None and (x.shape != t.shape or x.dtype != t.dtype):
+            raise HdtError(-1, "tensors of one call must have the same shape and type")
+
+
+def _rows(x):
+    """(rows, columns, type): all dimensions but the last are rows."""
+    if x.dim() < 1 or x.dtype not in _DTYPES:
+        raise HdtError(-3, "rows must be float32 or bfloat16")
+    return (x.numel() // x.shape[-1] if x.shape[-1] else 0), x.shape[-1], _DTYPES[x.dtype]
+
+
+def hdt_dropout(x, p, rng, site=0, residual=None, out=None):
+    """residual + D o x for x [..., cols], D the scaled keep mask of (rng, site): rng is a CUDA int64 tensor [2] = seed,
+    offset.  The gradient with respect to x is the same call on the gradient of the result, without a residual."""
+    rows, cols, dt = _rows(x)
+    if rng is None:
+        raise HdtError(-1, "hdt_dropout: p > 0 needs the generator's state")
+    y = torch.empty_like(x) if out is None else out
+    _here(x, residual, y)
+    _like(x, residual, y)
+    rc = (_lib or lib()).hdt_dropout(x.data_ptr(), _ptr(residual), _rng(rng, p), int(site), rows, cols, dt, float(p), y.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return y
+
+
+def _norm_weights(cols, *weights):
+    for w in weights:
+        if w.numel() != cols or w.dtype not in _DTYPES or w.dtype != weights[0].dtype:
+            raise HdtError(-1, "weight and bias must have one element per column and one type")
+
+
+def hdt_layer_norm_fwd(x, weight, bias, eps=1e-5, residual=None, p=0.0, rng=None, site=0, h=None, out=None, mean=None, rstd=None):
+    """h = residual + D o x, y = layer norm of h over the last dimension.  Returns (y, h, mean, rstd); h is x itself
+    without a residual and without dropout."""
+    rows, cols, dt = _rows(x)
+    y = torch.empty_like(x) if out is None else out
+    changed = residual is not None or p > 0
+    if h is None and changed:
+        h = torch.empty_like(x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+    _here(x, residual, y, h, mean, rstd, weight, bias)
+    _like(x, residual, y, h)
+    _norm_weights(cols, weight, bias)
+    if mean.numel() != rows or rstd.numel() != rows or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
+        raise HdtError(-1, "mean and rstd must be float32, one element per row")
+    rc = (_lib or lib()).hdt_layer_norm_fwd(x.data_ptr(), _ptr(residual), weight.data_ptr(), bias.data_ptr(), _rng(rng, p), int(site), float(p), rows, cols, dt,
+                                            _DTYPES[weight.dtype], float(eps), _ptr(h), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream())
+    if rc:
+        _check(rc)
+    return y, (x if h is None else h), mean, rstd
+
+
+@functools.lru_cache(maxsize=256)
+def hdt_layer_norm_workspace_bytes(rows, cols) -> int:
+    return int(lib().hdt_layer_norm_workspace_bytes(rows, cols))
+
+
+def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, site=0, d_residual=None, d_x=None, d_weight=None, d_bias=None,
+                       workspace=None):
+    """Gradients (d_x, d_residual, d_weight, d_bias) of hdt_layer_norm_fwd; d_h is the gradient that h gets from elsewhere.
+    Without dropout d_x and d_residual are one tensor."""
+    rows, cols, dt = _rows(h)
+    d_residual = torch.empty_like(h) if d_residual is None else d_residual
+    if p > 0 and d_x is None:
+        d_x = torch.empty_like(h)
+    d_weight = torch.empty_like(weight) if d_weight is None else d_weight
+    d_bias = torch.empty_like(weight) if d_bias is None else d_bias
+    if workspace is None:
+        workspace = torch.empty(max(hdt_layer_norm_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=h.device)
+    _here(d_y, d_h, h, d_residual, d_x, mean, rstd, weight, d_weight, d_bias, workspace)
+    _like(h, d_y, d_h, d_residual, d_x)
+    _norm_weights(cols, weight, d_weight, d_bias)
+    if mean.numel() != rows or rstd.numel() != rows or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
+        raise HdtError(-1, "mean and rstd must be float32, one element per row")
+    rc = (_lib or lib()).hdt_layer_norm_bwd(d_y.data_ptr(), _ptr(d_h), h.data_ptr(), mean.data_ptr(), rstd.data_ptr(), weight.data_ptr(), _rng(rng, p), int(site),
+                                            float(p), rows, cols, dt, _DTYPES[weight.dtype], d_residual.data_ptr(), _ptr(d_x), d_weight.data_ptr(), d_bias.data_ptr(),
+                                            workspace.data_ptr(), workspace.numel(), _stream())
+    if rc:
+        _check(rc)
+    return (d_residual if d_x is None else d_x), d_residual, d_weight, d_bias
 
 
 def hdt_set_option(name: str, value: int) -> None:
