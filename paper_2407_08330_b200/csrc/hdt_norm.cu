@@ -21,7 +21,7 @@
 namespace hdt {
 namespace {
 
-constexpr int THREADS = 128;
+constexpr int THREADS = 128, BWD_CTAS = 4;
 
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS) k_norm_fwd(const
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
-__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS) k_norm_bwd(const NormArgs a) {
+__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : BWD_CTAS) k_norm_bwd(const NormArgs a) {
     constexpr int NW = WPR > 4 ? WPR : THREADS / 32, RPC = WPR > 1 ? 1 : NW * (32 / LPR);   // rows of a CTA at a time
     __shared__ float s_sum[WPR];
     __shared__ float s_col[WPR > 1 ? 1 : NW * 8 * 32];
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(1024) k_norm_columns(const float *part, int n,
 }
 
 template <typename T, bool VEC, int LPR>
-__global__ void __launch_bounds__(256) k_dropout(const T *x, const T *residual, T *y, int rows, int cols, const Drop d) {
+__global__ void __launch_bounds__(256, 4) k_dropout(const T *x, const T *residual, T *y, int rows, int cols, const Drop d) {
     constexpr int U = 4;
     const int lane = threadIdx.x & 31, l = lane % LPR;
     const int first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / LPR) + lane / LPR;
@@ -241,22 +241,24 @@ __global__ void __launch_bounds__(256) k_dropout(const T *x, const T *residual, 
     const int chunks = (cols + 8 * LPR - 1) / (8 * LPR);
     const PhiloxKey k = philox_key(d);
     for (int c0 = 0; c0 < chunks; c0 += U) {
-        float v[U][8], r[U][8];
+        Raw8<T, VEC> rx[U], rr[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (c0 + i < chunks) load8<LPR, VEC>(x + at, c0 + i, l, cols, v[i]);
-            if (c0 + i < chunks && residual != nullptr) load8<LPR, VEC>(residual + at, c0 + i, l, cols, r[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) r[i][e] = 0.f;
+        for (int i = 0; i < U; ++i) {      // (a chunk behind the row's end reads as zeros)
+            rx[i].template load<LPR>(x + at, c0 + i, l, cols);
+            if (residual != nullptr) rr[i].template load<LPR>(residual + at, c0 + i, l, cols);
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             if (c0 + i >= chunks) break;
-            drop8<LPR, VEC>(k, d, row, c0 + i, l, v[i]);
+            float v[8], r[8];
+            rx[i].get(v);
+            drop8<LPR, VEC>(k, d, row, c0 + i, l, v);
+            if (residual != nullptr) {
+                rr[i].get(r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] += r[i][e];
-            if (on) store8<LPR, VEC>(y + at, c0 + i, l, cols, v[i]);
+                for (int e = 0; e < 8; ++e) v[e] += r[e];
+            }
+            if (on) store8<LPR, VEC>(y + at, c0 + i, l, cols, v);
         }
     }
 }
@@ -311,7 +313,7 @@ int norm_types(const NormArgs &a, int dtype, int w_dtype, bool vec, cudaStream_t
 int rows_at_once(int cols) { return cols > 1024 ? 1 : cols > 128 ? 4 : cols > 64 ? 8 : cols > 32 ? 16 : 32; }
 // CTAs of the backward, and so partial rows: at most four to an SM.
 int bwd_grid(int64_t rows, int cols) {
-    const int64_t need = (rows + rows_at_once(cols) - 1) / rows_at_once(cols), most = cols > 4096 ? PLAN_SMS : 4 * PLAN_SMS;
+    const int64_t need = (rows + rows_at_once(cols) - 1) / rows_at_once(cols), most = cols > 4096 ? PLAN_SMS : BWD_CTAS * PLAN_SMS;
     return (int)(need < most ? need : most);
 }
 

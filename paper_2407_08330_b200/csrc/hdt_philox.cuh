@@ -48,34 +48,67 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162flo
 __device__ __forceinline__ void from_f32(float &d, float x) { d = x; }
 __device__ __forceinline__ void from_f32(__nv_bfloat16 &d, float x) { d = __float2bfloat16(x); }
 
-// Columns that the row does not have read as 0.  (VEC rows have a multiple of eight columns.)
-template <int LPR, bool VEC, typename T>
-__device__ __forceinline__ void load8(const T *row, int chunk, int l, int cols, float (&v)[8]) {
-    if constexpr (VEC) {
+// A lane's eight columns of a chunk as they are in memory: what has been requested and is not needed yet takes half of
+// the registers of its values in fp32 (bf16).  Columns that the row does not have read as 0.  (VEC rows have a
+// multiple of eight columns.)
+template <typename T, bool VEC>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16, true> {
+    uint4 x;
+    template <int LPR>
+    __device__ __forceinline__ void load(const __nv_bfloat16 *row, int chunk, int l, int cols) {
         const int c = col_of<LPR, true>(chunk, l, 0);
-        if (c >= cols) {
+        x = c < cols ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        } else if constexpr (sizeof(T) == 2) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(row + c);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[2 * e] = __uint_as_float(w[e] << 16);
-                v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-            }
-        } else {
-            const float4 x = *reinterpret_cast<const float4 *>(row + c), y = *reinterpret_cast<const float4 *>(row + c + 4);
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-            v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
         }
-    } else {
+    }
+};
+template <>
+struct Raw8<float, true> {
+    float4 x, y;
+    template <int LPR>
+    __device__ __forceinline__ void load(const float *row, int chunk, int l, int cols) {
+        const int c = col_of<LPR, true>(chunk, l, 0);
+        x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < cols) {
+            x = *reinterpret_cast<const float4 *>(row + c);
+            y = *reinterpret_cast<const float4 *>(row + c + 4);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    }
+};
+template <typename T>
+struct Raw8<T, false> {
+    T x[8];
+    template <int LPR>
+    __device__ __forceinline__ void load(const T *row, int chunk, int l, int cols) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int c = col_of<LPR, false>(chunk, l, e);
-            v[e] = c < cols ? to_f32(row[c]) : 0.f;
+            if (c < cols) x[e] = row[c];
+            else from_f32(x[e], 0.f);
         }
     }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = to_f32(x[e]);
+    }
+};
+template <int LPR, bool VEC, typename T>
+__device__ __forceinline__ void load8(const T *row, int chunk, int l, int cols, float (&v)[8]) {
+    Raw8<T, VEC> r;
+    r.template load<LPR>(row, chunk, l, cols);
+    r.get(v);
 }
 template <int LPR, bool VEC, typename T>
 __device__ __forceinline__ void store8(T *row, int chunk, int l, int cols, const float (&v)[8]) {
