@@ -352,6 +352,48 @@ int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const fl
                        void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Self-attention of packed documents with a learned bias for each bucket of relative positions: the decoder's
+ * sub-layer of the paper's encoder-decoder model (paragraph "Hierarchical Encoder and Decoder Stacks"; causal), or a
+ * dense encoder's (not causal).  For row i of document b, whose n_q rows of q are the last ones of its n_k positions,
+ *     pos_i = n_k - n_q + i,  d = pos_i - j for key j,   A_ij = softmax_scale q_i . k_j + bias[bucket(d)][head],
+ *     O = softmax(A) V over the document's keys (causal: those with d >= 0),   LSE_i = log sum_j exp(A_ij).
+ * A row without a key (no keys, or causal and pos_i < 0) gets O = 0, LSE = -inf and zero gradients.
+ * Buckets: with n = num_buckets (causal; keys behind the query do not count) or n = num_buckets / 2 for each direction
+ * (not causal; the second half is that of d < 0), e = n / 2 rounded down and x = |d|:
+ *     bucket = x for x < e, else min(n - 1, e + floor((n - e) ln(x / e) / ln(max_distance / e))),
+ * exact where the quotient is whole.
+ *   cu_seqlens_q, cu_seqlens_k   device int32 [batch + 1]: a document's rows of q, and of k and v
+ *   seqlens_k          device int32 [batch] or NULL: n_k, where a document's part of k and v has room behind its keys
+ *                      (a cache); what lies there may hold anything
+ *   q, o, d_o, dq      device [total_q, heads, head_dim] of `dtype`, 16-byte aligned
+ *   k, v, dk, dv       device [total_k, heads, head_dim]
+ *   bias, d_bias       device [num_buckets, heads] of `dtype`; bias NULL: none (num_buckets, max_distance and d_bias
+ *                      are not looked at).  Finite entries beyond +-30000 count as +-30000; -inf shuts a bucket out
+ *   lse                device float [heads, total_q]
+ *   workspace          device, >= hdt_self_workspace_bytes(..., bwd), 256-byte aligned; scratch.  num_buckets 0: no bias
+ * 2 <= n, num_buckets <= 128 and even if not causal, n / 2 < max_distance <= 32768.  head_dim 64 or 128; softmax_scale <= 0
+ * means 1/sqrt(head_dim).  Rows that belong to no document, and k and v's beyond n_k, are left as they were in o, lse and
+ * the gradients.  Offsets outside [0, total] are clamped; documents that overlap are not written whole.  bf16: a row of a document
+ * that is not finite reaches the document's other rows of its tile; other documents never do.
+ * Backward: dS = P o (d_o V^T - delta), dQ = scale dS K, dK = scale dS^T Q, dV = P^T d_o, d_bias[u][h] = sum of dS over the
+ * pairs of bucket u (all documents); nothing is summed in an order that changes from run to run.
+ * A call whose total_q is at most 4 x batch is taken as a step of autoregressive decoding (few rows a document, keys
+ * split among warps).  Asynchronous on `stream`, no host wait; the offsets are read on the device only.
+ */
+size_t hdt_self_workspace_bytes(int32_t batch, int32_t total_q, int32_t total_k, int32_t heads, int32_t head_dim,
+                                int32_t num_buckets, int32_t max_distance, int32_t causal, int32_t dtype, int32_t bwd);
+int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch,
+                      int32_t total_q, int32_t total_k, const void *q, const void *k, const void *v, const void *bias,
+                      int32_t num_buckets, int32_t max_distance, int32_t causal, void *o, float *lse, int32_t heads,
+                      int32_t head_dim, int32_t dtype, float softmax_scale, void *workspace, size_t workspace_bytes,
+                      void *stream);
+int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch,
+                      int32_t total_q, int32_t total_k, const void *q, const void *k, const void *v, const void *bias,
+                      int32_t num_buckets, int32_t max_distance, int32_t causal, const void *o, const float *lse,
+                      const void *d_o, void *dq, void *dk, void *dv, void *d_bias, int32_t heads, int32_t head_dim,
+                      int32_t dtype, float softmax_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Waits for `stream`, then returns and clears the first failure a kernel of this library
  * recorded on the device: HDT_ERR_TIMEOUT when a bounded wait (on a TMA or tensor-core
  * completion barrier) ran out; results of that call are then undefined.  HDT_OK if none.

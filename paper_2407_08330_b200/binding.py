@@ -87,6 +87,14 @@ def lib():
         L.hdt_layer_norm_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
         L.hdt_layer_norm_bwd.restype = C.c_int
         L.hdt_layer_norm_bwd.argtypes = [C.c_void_p] * 7 + [C.c_int32, C.c_float, C.c_int64] + [C.c_int32] * 3 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        L.hdt_self_workspace_bytes.restype = C.c_size_t
+        L.hdt_self_workspace_bytes.argtypes = [C.c_int32] * 10
+        L.hdt_self_attn_fwd.restype = C.c_int
+        L.hdt_self_attn_fwd.argtypes = [C.c_void_p] * 3 + [C.c_int32] * 3 + [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_void_p] * 2 + [C.c_int32] * 3 + \
+                                       [C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.hdt_self_attn_bwd.restype = C.c_int
+        L.hdt_self_attn_bwd.argtypes = [C.c_void_p] * 3 + [C.c_int32] * 3 + [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_void_p] * 7 + [C.c_int32] * 3 + \
+                                       [C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
         L.hdt_set_option.restype = C.c_int
         L.hdt_device_status.restype = C.c_int
         L.hdt_device_status.argtypes = [C.c_void_p]
@@ -461,6 +469,73 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
     if rc:
         _check(rc)
     return (d_residual if d_x is None else d_x), d_residual, d_weight, d_bias
+
+
+@functools.lru_cache(maxsize=256)
+def hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, bwd) -> int:
+    return int(lib().hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, int(causal), _DTYPES[dtype], int(bwd)))
+
+
+def _self_common(cu_q, cu_k, seqlens_k, q, k, v, bias):
+    if q.dim() != 3 or q.dtype not in _DTYPES or k.shape[1:] != q.shape[1:] or k.dtype != q.dtype:
+        raise HdtError(-1, "q, k and v must be [rows, heads, head_dim], float32 or bfloat16 alike")
+    _like(k, v)
+    B = cu_q.numel() - 1
+    for t, n in ((cu_q, B + 1), (cu_k, B + 1), (seqlens_k, B)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != n):
+            raise HdtError(-1, "offsets must be int32 [batch + 1], lengths int32 [batch]")
+    if bias is not None and (bias.dim() != 2 or bias.shape[1] != q.shape[1] or bias.dtype != q.dtype):
+        raise HdtError(-1, "bias must be [num_buckets, heads] of q's type")
+    return B, q.shape[0], k.shape[0], q.shape[1], q.shape[2], (0 if bias is None else bias.shape[0])
+
+
+def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distance=128, causal=True, softmax_scale=0.0, seqlens_k=None, out=None,
+                      lse=None, workspace=None):
+    """Self-attention of packed documents with a bias [num_buckets, heads] by relative position: q [Tq,H,d] (the last rows
+    of every document), k, v [Tk,H,d]; seqlens_k [batch] where a document's part of k and v has room behind its keys (a
+    cache).  Returns (O [Tq,H,d], LSE [H,Tq])."""
+    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
+    out = torch.empty_like(q) if out is None else out
+    lse = torch.empty((H, Tq), dtype=torch.float32, device=q.device) if lse is None else lse
+    if workspace is None:
+        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, False)), dtype=torch.uint8, device=q.device)
+    _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, out, lse, workspace)
+    _like(q, out)
+    if lse.shape != (H, Tq) or lse.dtype != torch.float32:
+        raise HdtError(-1, "lse must be float32 [heads, rows of q]")
+    rc = (_lib or lib()).hdt_self_attn_fwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                           _ptr(bias), n, int(max_distance), int(bool(causal)), out.data_ptr(), lse.data_ptr(), H, d, _DTYPES[q.dtype],
+                                           float(softmax_scale), workspace.data_ptr(), workspace.numel(), _stream())
+    if rc:
+        _check(rc)
+    return out, lse
+
+
+def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=None, max_distance=128, causal=True, softmax_scale=0.0, seqlens_k=None,
+                      dq=None, dk=None, dv=None, d_bias=None, workspace=None):
+    """Gradients (dQ, dK, dV, dBias) of hdt_self_attn_fwd; dBias is None without a bias."""
+    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(k) if dv is None else dv
+    if bias is not None and d_bias is None:
+        d_bias = torch.empty_like(bias)
+    if workspace is None:
+        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, True)), dtype=torch.uint8, device=q.device)
+    _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, o, lse, d_o, dq, dk, dv, d_bias, workspace)
+    _like(q, o, d_o, dq)
+    _like(k, dk, dv)
+    if bias is not None:
+        _like(bias, d_bias)
+    if lse.shape != (H, Tq) or lse.dtype != torch.float32:
+        raise HdtError(-1, "lse must be float32 [heads, rows of q]")
+    rc = (_lib or lib()).hdt_self_attn_bwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                           _ptr(bias), n, int(max_distance), int(bool(causal)), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(), dq.data_ptr(),
+                                           dk.data_ptr(), dv.data_ptr(), _ptr(d_bias), H, d, _DTYPES[q.dtype], float(softmax_scale), workspace.data_ptr(),
+                                           workspace.numel(), _stream())
+    if rc:
+        _check(rc)
+    return dq, dk, dv, (None if bias is None else d_bias)
 
 
 def hdt_set_option(name: str, value: int) -> None:

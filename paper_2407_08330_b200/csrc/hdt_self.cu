@@ -1,0 +1,613 @@
+// Self-attention with a learned relative position bias: C entry points, what a call prepares on the device, the step of
+// autoregressive decoding, and the last sum of the bias' gradient.
+//
+// Preparation (one launch): the documents' blocks of rows, ordered by cost (a persistent kernel takes the dearest
+// first), from offsets that only the device knows; and the bias by distance, [heads][distances], so that a tile reads a
+// vector of it and nobody looks for buckets again.  Latency: 4 x 4096 tokens about 5 us.
+//
+// Decoding (few rows per document): bound by HBM, the keys and values once.  A warp takes a piece of a document's keys for
+// one head and up to four rows; a key is read by D / 8 (bf16) or D / 4 (fp32) lanes, 16 bytes each, four keys per lane
+// group in flight; every lane group has a softmax of its own, joined at the piece's end, the pieces by k_self_join.
+// A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
+#include <math.h>
+
+#include "hdt_self.cuh"
+
+namespace hdt {
+namespace {
+
+struct PrepList { SelfBlk *raw, *out; int *count; int rows, of_keys, most; };
+struct PrepArgs {
+    const int32_t *cu_q, *cu_k, *len_k;
+    int B, Tq, Tk, H, n_lists;
+    PrepList list[2];
+    SelfRel rel;
+    const void *table;
+    int dtype;
+    float *bias;
+    unsigned char *bucket;
+    int lo, n;
+};
+// A document's rows, whatever the arrays hold: inside the tensors, never negative.
+struct Doc { int q0, nq, k0, nk; };
+__device__ __forceinline__ Doc document(const int32_t *cu_q, const int32_t *cu_k, const int32_t *len_k, int b, int Tq, int Tk) {
+    Doc d;
+    d.q0 = min(max(cu_q[b], 0), Tq);
+    d.nq = min(max(cu_q[b + 1], d.q0), Tq) - d.q0;
+    d.k0 = min(max(cu_k[b], 0), Tk);
+    d.nk = min(max(cu_k[b + 1], d.k0), Tk) - d.k0;
+    if (len_k != nullptr) d.nk = min(max(len_k[b], 0), d.nk);
+    return d;
+}
+__device__ __forceinline__ float load_f32(const void *p, size_t i, int dtype) {
+    return dtype == HDT_F32 ? ((const float *)p)[i] : __bfloat162float(((const __nv_bfloat16 *)p)[i]);
+}
+__device__ __forceinline__ float bias_base2(const void *table, size_t i, int dtype) {
+    const float v = load_f32(table, i, dtype);
+    return (isfinite(v) ? fminf(fmaxf(v, -SELF_MAX_BIAS), SELF_MAX_BIAS) : v) * 1.4426950408889634f;
+}
+
+// Inclusive scan over the CTA's 1024 threads.
+__device__ __forceinline__ int scan1024(int v, int *s_warp) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += y;
+    }
+    if (lane == 31) s_warp[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+        int w = s_warp[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += y;
+        }
+        s_warp[lane] = w;
+    }
+    __syncthreads();
+    v += warp > 0 ? s_warp[warp - 1] : 0;
+    __syncthreads();
+    return v;
+}
+
+__global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ PrepArgs a) {
+    constexpr int BINS = 1024;
+    __shared__ int s_warp[32], s_pre[1024], s_bin[BINS];
+    const int t = threadIdx.x;
+    pdl_launch_dependents();
+    if ((int)blockIdx.x >= a.n_lists) {      // the bias by distance
+        const int i = ((int)blockIdx.x - a.n_lists) * 1024 + t;
+        if (i >= a.n) return;
+        const int bk = self_bucket(a.rel, a.lo + i);
+        a.bucket[i] = (unsigned char)bk;
+        for (int h = 0; h < a.H; ++h) a.bias[(size_t)h * a.n + i] = bias_base2(a.table, (size_t)bk * a.H + h, a.dtype);
+        return;
+    }
+    const PrepList L = a.list[blockIdx.x];
+    s_bin[t] = 0;
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 1024) {
+        int nb = 0;
+        if (b0 + t < a.B) {
+            const Doc d = document(a.cu_q, a.cu_k, a.len_k, b0 + t, a.Tq, a.Tk);
+            nb = ((L.of_keys ? d.nk : d.nq) + L.rows - 1) / L.rows;
+        }
+        s_pre[t] = scan1024(nb, s_warp);
+        __syncthreads();
+        const int n = s_pre[1023];
+        for (int i = t; i < n; i += 1024) {
+            int lo = 0, hi = 1023;           // first document whose blocks end behind i
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (s_pre[mid] > i) hi = mid;
+                else lo = mid + 1;
+            }
+            const Doc d = document(a.cu_q, a.cu_k, a.len_k, b0 + lo, a.Tq, a.Tk);
+            SelfBlk x;
+            x.q0 = d.q0; x.nq = d.nq; x.k0 = d.k0; x.nk = d.nk; x.off = d.nk - d.nq;
+            x.r0 = (i - (lo > 0 ? s_pre[lo - 1] : 0)) * L.rows;
+            x.tiles = L.of_keys ? (d.nq - self_first_row(a.rel.causal, x.r0, d.nq, d.nk) + 127) >> 7 : (self_keys_of(a.rel.causal, x.r0, L.rows, d.nq, d.nk) + 127) >> 7;
+            x.id = total + i;
+            if (x.id >= L.most) break;       // (documents that overlap: there is room for those that do not)
+            L.raw[x.id] = x;
+            atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1);
+        }
+        total += n;
+        __syncthreads();
+    }
+    total = min(total, L.most);
+    const int mine = s_bin[t];
+    const int start = scan1024(mine, s_warp) - mine;      // (its barriers lie between the last read and the next write)
+    s_bin[t] = start;
+    __syncthreads();
+    for (int i = t; i < total; i += 1024) {
+        const SelfBlk x = L.raw[i];
+        L.out[atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1)] = x;
+    }
+    if (t == 0) *L.count = total;
+}
+
+// Sums of the blocks' partial sums, a CTA per head; threads of one bucket take every G-th block, then meet in order.
+__global__ void __launch_bounds__(1024) k_self_dbias(const float *part, const int *count, int H, int buckets, int dtype, void *out) {
+    __shared__ float s[1024];
+    const int h = blockIdx.x, G = 1024 / buckets, b = threadIdx.x % buckets, g = threadIdx.x / buckets;
+    pdl_wait();
+    const int n = part != nullptr ? *count : 0;
+    float v = 0.f;
+    if (g < G)
+#pragma unroll 4
+        for (int i = g; i < n; i += G) v += part[((size_t)i * H + h) * buckets + b];
+    s[threadIdx.x] = v;
+    __syncthreads();
+    if (g != 0) return;
+    for (int i = 1; i < G; ++i) v += s[i * buckets + b];
+    if (dtype == HDT_F32) ((float *)out)[(size_t)b * H + h] = v;
+    else ((__nv_bfloat16 *)out)[(size_t)b * H + h] = __float2bfloat16(v);
+}
+
+// ---- decoding -----------------------------------------------------------------------------------
+struct StepArgs {
+    const int32_t *cu_q, *cu_k, *len_k;
+    int B, Tq, Tk, H, piece, dtype, items;      // items: an upper limit
+    const void *q, *k, *v, *table;
+    void *o;
+    float *lse, *part_o, *part_ml;      // [slot][H][D], [slot][H][2]; a slot per (item, row of its group)
+    float scale_log2;
+    SelfRel rel;
+};
+template <int RG>
+struct StepDoc {      // how a document's work is cut: row groups x pieces of keys
+    int groups, per, pieces;
+    __device__ __forceinline__ StepDoc(const Doc &d, int piece) {
+        groups = (d.nq + RG - 1) / RG;
+        per = piece * groups;
+        pieces = groups == 0 ? 0 : max(1, (d.nk + per - 1) / per);
+    }
+    __device__ __forceinline__ int items() const { return groups * pieces; }
+};
+// The document that item x, or row x, lies in, and how many items come before the document (whole warp).
+template <int RG, bool BY_ROW>
+__device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &before) {
+    const int lane = threadIdx.x & 31;
+    int base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        Doc m{0, 0, 0, 0};
+        if (b0 + lane < a.B) m = document(a.cu_q, a.cu_k, a.len_k, b0 + lane, a.Tq, a.Tk);
+        const int n = StepDoc<RG>(m, a.piece).items();
+        int pre = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, pre, o);
+            if (lane >= o) pre += y;
+        }
+        const int first = base + pre - n;
+        const unsigned hit = __ballot_sync(0xffffffffu, n > 0 && (BY_ROW ? x >= m.q0 && x < m.q0 + m.nq : x >= first && x < first + n));
+        if (hit) {
+            const int src = __ffs(hit) - 1;
+            d.q0 = __shfl_sync(0xffffffffu, m.q0, src);
+            d.nq = __shfl_sync(0xffffffffu, m.nq, src);
+            d.k0 = __shfl_sync(0xffffffffu, m.k0, src);
+            d.nk = __shfl_sync(0xffffffffu, m.nk, src);
+            before = __shfl_sync(0xffffffffu, first, src);
+            return true;
+        }
+        base += __shfl_sync(0xffffffffu, pre, 31);
+    }
+    return false;
+}
+template <bool BF16>
+struct Vec16 {      // 16 bytes of a row
+    static constexpr int E = BF16 ? 8 : 4;
+    uint4 x;
+    __device__ __forceinline__ void load(const void *p, size_t row16) { x = reinterpret_cast<const uint4 *>(p)[row16]; }
+    __device__ __forceinline__ float get(int e) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        if constexpr (BF16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else return __uint_as_float(w[e]);
+    }
+};
+
+template <int D, bool BF16, int RG>
+__global__ void __launch_bounds__(128) k_self_step(const __grid_constant__ StepArgs a) {
+    using V = Vec16<BF16>;
+    constexpr int E = V::E, LPK = D / E, KPI = 32 / LPK, U = 4;
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, l = lane % LPK, slot = lane / LPK;
+    const int wid = blockIdx.x * 4 + (threadIdx.x >> 5), item = wid / a.H, h = wid % a.H;
+    Doc d;
+    int before;
+    if (item >= a.items || !find_doc<RG, false>(a, item, d, before)) return;
+    const StepDoc<RG> cut(d, a.piece);
+    const int g = (item - before) / cut.pieces, pc = (item - before) % cut.pieces, r0 = g * RG, nr = min(RG, d.nq - r0);
+    const int pos0 = d.nk - d.nq + r0;                                  // position of the group's first row
+    const int kb = min(pc * cut.per, d.nk);
+    int ke = min(kb + cut.per, d.nk);
+    if (a.rel.causal) ke = max(kb, min(ke, pos0 + nr));
+    float q[RG][E], acc[RG][E], m[RG], s_l[RG];
+#pragma unroll
+    for (int r = 0; r < RG; ++r) {
+        V x;
+        x.load(a.q, ((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * LPK + l);
+        m[r] = -INFINITY;
+        s_l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            q[r][e] = x.get(e) * a.scale_log2;
+            acc[r][e] = 0.f;
+        }
+    }
+    const float far_bias = a.rel.on ? bias_base2(a.table, (size_t)self_bucket(a.rel, a.rel.far) * a.H + h, a.dtype) : 0.f;
+    for (int k0 = kb; k0 < ke; k0 += KPI * U) {
+        V kx[U], vx[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const size_t row = ((size_t)(d.k0 + min(k0 + u * KPI + slot, ke - 1)) * a.H + h) * LPK + l;
+            kx[u].load(a.k, row);
+            vx[u].load(a.v, row);
+        }
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+            if (r > 0 && r >= nr) break;
+            float s[U], top = m[r];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s[u] = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[u] = fmaf(q[r][e], kx[u].get(e), s[u]);
+            }
+#pragma unroll
+            for (int o = LPK / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int u = 0; u < U; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int key = k0 + u * KPI + slot, dist = pos0 + r - key;
+                if (a.rel.on) s[u] += dist >= a.rel.far ? far_bias : bias_base2(a.table, (size_t)self_bucket(a.rel, dist) * a.H + h, a.dtype);
+                if (key >= ke || (a.rel.causal && dist < 0)) s[u] = -INFINITY;
+                top = fmaxf(top, s[u]);
+            }
+            const float use = top == -INFINITY ? 0.f : top, f = exp2f(m[r] - use);
+            m[r] = top;
+            s_l[r] *= f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[r][e] *= f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float p = exp2f(s[u] - use);
+                s_l[r] += p;
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(p, vx[u].get(e), acc[r][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RG; ++r) {
+        if (r > 0 && r >= nr) break;
+#pragma unroll
+        for (int o = LPK; o < 32; o <<= 1) {      // the lane groups' softmaxes
+            const float m2 = __shfl_xor_sync(0xffffffffu, m[r], o), top = fmaxf(m[r], m2), use = top == -INFINITY ? 0.f : top;
+            const float f = exp2f(m[r] - use), f2 = exp2f(m2 - use);
+            s_l[r] = s_l[r] * f + __shfl_xor_sync(0xffffffffu, s_l[r], o) * f2;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[r][e] = acc[r][e] * f + __shfl_xor_sync(0xffffffffu, acc[r][e], o) * f2;
+            m[r] = top;
+        }
+        if (lane >= LPK) continue;
+        const int row = d.q0 + r0 + r;
+        if (cut.pieces == 1) {
+            const float inv = s_l[r] == 0.f ? 0.f : 1.f / s_l[r];
+            const size_t at = ((size_t)row * a.H + h) * D + l * E;
+            if constexpr (BF16) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(acc[r][2 * e] * inv, acc[r][2 * e + 1] * inv);
+                    w[e] = *reinterpret_cast<const uint32_t *>(&p);
+                }
+                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.o + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else *reinterpret_cast<float4 *>((float *)a.o + at) = make_float4(acc[r][0] * inv, acc[r][1] * inv, acc[r][2] * inv, acc[r][3] * inv);
+            if (l == 0) a.lse[(size_t)h * a.Tq + row] = s_l[r] == 0.f ? -INFINITY : (m[r] + log2f(s_l[r])) * 0.6931471805599453f;
+        } else {
+            const size_t at = ((size_t)item * RG + r) * a.H + h;
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<float4 *>(a.part_o + at * D + l * E + e) = make_float4(acc[r][e], acc[r][e + 1], acc[r][e + 2], acc[r][e + 3]);
+            if (l == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(m[r], s_l[r]);
+        }
+    }
+}
+
+// The pieces of a row, a warp per (row, head).
+template <int D, bool BF16, int RG>
+__global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepArgs a) {
+    constexpr int E = D / 32;
+    const int lane = threadIdx.x & 31, wid = blockIdx.x * 4 + (threadIdx.x >> 5), row = wid / a.H, h = wid % a.H;
+    Doc d;
+    int before;
+    // (before the wait: the kernel in front does not write the offsets, and began behind what did)
+    const bool found = row < a.Tq && find_doc<RG, true>(a, row, d, before);
+    pdl_wait();
+    if (!found) return;
+    const StepDoc<RG> cut(d, a.piece);
+    const int r = row - d.q0, first = before + (r / RG) * cut.pieces;
+    if (cut.pieces == 1 || first + cut.pieces > a.items) return;      // written by the one warp that had the row (or no valid offsets)
+    auto at = [&](int i) { return ((size_t)(first + i) * RG + r % RG) * a.H + h; };
+    float top = -INFINITY;
+    for (int i = lane; i < cut.pieces; i += 32) top = fmaxf(top, a.part_ml[at(i) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float use = top == -INFINITY ? 0.f : top;
+    float l = 0.f, acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < cut.pieces; ++i) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2);
+        const float f = exp2f(ml.x - use);
+        l += ml.y * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(a.part_o[at(i) * D + lane * E + e], f, acc[e]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const size_t out = ((size_t)row * a.H + h) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if constexpr (BF16) ((__nv_bfloat16 *)a.o)[out + e] = __float2bfloat16(acc[e] * inv);
+        else ((float *)a.o)[out + e] = acc[e] * inv;
+    }
+    if (lane == 0) a.lse[(size_t)h * a.Tq + row] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+// Whether the distance d has passed the border far^(k/m) e^(1 - k/m), i.e. d^m e^k >= far^k e^m.  The difference of
+// the logarithms is known to about 1e-15 of their size; where it is that small, the two products are compared by their prime
+// factors.
+bool same_product(int d, int m, int far, int k, int e) {      // d^m e^(k - m) == far^k ?
+    for (int p = 2; d > 1 || far > 1 || e > 1; ++p) {
+        if ((long long)p * p > (d > far ? (d > e ? d : e) : (far > e ? far : e))) p = d > 1 ? d : far > 1 ? far : e;
+        long long n = 0;
+        while (d % p == 0) { d /= p; n += m; }
+        while (e % p == 0) { e /= p; n += k - m; }
+        while (far % p == 0) { far /= p; n -= k; }
+        if (n != 0) return false;
+    }
+    return true;
+}
+bool passed(int d, int m, int far, int k, int e) {
+    const double x = m * log((double)d) + (k - m) * log((double)e) - k * log((double)far);
+    return x > 1e-9 || (x > -1e-9 && (same_product(d, m, far, k, e) || x > 0));
+}
+// The buckets of one direction: one per distance below half of them, then logarithmic up to max_distance.
+void rel_fill(SelfRel *r, int buckets, int max_distance, int causal) {
+    static thread_local SelfRel last{};
+    static thread_local int last_far = -1;
+    if (last_far == max_distance && last.buckets == buckets && last.causal == causal) { *r = last; return; }
+    SelfRel x{};
+    x.on = 1; x.causal = causal; x.buckets = buckets; x.one_way = causal ? buckets : buckets / 2;
+    const int e = x.one_way / 2, m = x.one_way - e;
+    for (int b = 0; b <= e; ++b) x.first[b] = b;
+    for (int k = 1; k < m; ++k) {
+        int d = (int)(e * pow((double)max_distance / e, (double)k / m)) - 1;
+        if (d < x.first[e + k - 1]) d = x.first[e + k - 1];
+        while (!passed(d, m, max_distance, k, e)) ++d;
+        x.first[e + k] = d;
+    }
+    x.far = x.first[x.one_way - 1];
+    last = *r = x;
+    last_far = max_distance;
+}
+
+size_t al(size_t n) { return (n + 255) / 256 * 256; }
+constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which a call is a step of decoding
+bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
+// Keys of a piece: sixteen warps to an SM if the rows are one per document, at least 64.
+int step_piece(int Tk, int H) {
+    const long long per = ((long long)Tk * H + 16 * PLAN_SMS - 1) / (16 * PLAN_SMS);
+    return (int)((per < 64 ? 64 : per) + 15) / 16 * 16;
+}
+// (a document of g row groups has at most keys / piece + g items)
+long long step_items(int B, int Tq, int Tk, int H, int rg) { return (long long)Tk / step_piece(Tk, H) + Tq / rg + B + 2; }
+int step_group(int B, int Tq) { return Tq <= B ? 1 : STEP_ROWS; }
+
+struct Layout {
+    int rows_q, most_q, most_k, n;
+    size_t count, raw, q, k, bias, bucket, delta, part, part_o, part_ml, total;
+};
+long long blocks(int T, int B, int rows) { return (long long)T / rows + B; }
+Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance, int causal, int dtype, int bwd) {
+    Layout L{};
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t x = at; at += al(n); return x; };
+    if (!bwd && is_step(B, Tq)) {
+        const int rg = step_group(B, Tq);
+        const long long slots = step_items(B, Tq, Tk, H, rg) * rg;
+        L.part_o = take((size_t)slots * H * D * 4);
+        L.part_ml = take((size_t)slots * H * 8);
+    } else {
+        L.rows_q = dtype == HDT_F32 ? SELF_F32_ROWS : 128;
+        // two row tiles to a unit (they share the K and V tiles) where that leaves a unit for every SM
+        if (!bwd && dtype == HDT_BF16 && blocks(Tq, B, 256) * H >= PLAN_SMS) L.rows_q = 256;
+        L.most_q = (int)blocks(Tq, B, L.rows_q);
+        L.most_k = bwd ? (int)blocks(Tk, B, dtype == HDT_F32 ? SELF_F32_ROWS : 128) : 0;
+        L.count = take(8);
+        L.raw = take((size_t)(L.most_q + L.most_k) * sizeof(SelfBlk));
+        L.q = take((size_t)L.most_q * sizeof(SelfBlk));
+        L.k = take((size_t)L.most_k * sizeof(SelfBlk));
+        if (buckets > 0) {
+            L.n = causal ? max_distance + 1 : 2 * max_distance + 1;      // (an upper limit: the last border may lie before max_distance)
+            L.bias = take((size_t)L.n * H * 4);
+            L.bucket = take((size_t)L.n);
+        }
+        if (bwd) {
+            L.delta = take((size_t)H * Tq * 4);
+            if (buckets > 0) L.part = take((size_t)L.most_q * H * buckets * 4);
+        }
+    }
+    L.total = at > 0 ? at : 256;
+    return L;
+}
+int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance, int causal, int dtype, const char *who) {
+    if (B < 0 || Tq < 0 || Tk < 0 || H < 1 || buckets < 0) return set_error(HDT_ERR_INVALID_ARG, "%s: negative size or no head", who);
+    if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
+    if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
+    if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7fffff00LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
+    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7fffff00LL || step_items(B, Tq, Tk, H, 1) * H > 0x7fffff00LL)
+        return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
+    if (buckets > 0) {
+        const int one = causal ? buckets : buckets / 2;
+        if (buckets > SELF_MAX_BUCKETS) return set_error(HDT_ERR_UNSUPPORTED, "%s: at most %d buckets", who, SELF_MAX_BUCKETS);
+        if (one < 2 || (!causal && buckets % 2 != 0)) return set_error(HDT_ERR_INVALID_ARG, "%s: at least two buckets a direction, the same number both ways", who);
+        if (max_distance <= one / 2) return set_error(HDT_ERR_INVALID_ARG, "%s: max_distance must exceed half of a direction's buckets", who);
+        if (max_distance > SELF_MAX_DISTANCE) return set_error(HDT_ERR_UNSUPPORTED, "%s: max_distance at most %d", who, SELF_MAX_DISTANCE);
+    }
+    return HDT_OK;
+}
+int ptr_check(const void *p, const char *who) {
+    if (!p) return set_error(HDT_ERR_INVALID_ARG, "%s: null tensor pointer", who);
+    if ((uintptr_t)p & 15) return set_error(HDT_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    return HDT_OK;
+}
+int ws_check(const void *ws, size_t n, size_t need, const char *who) {
+    if (!ws || n < need) return set_error(HDT_ERR_WORKSPACE, "%s: workspace %zu < required %zu", who, n, need);
+    if ((uintptr_t)ws & 255) return set_error(HDT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+    return HDT_OK;
+}
+
+template <int D, bool BF16, int RG>
+int step_go(StepArgs a, cudaStream_t st) {
+    a.items = (int)step_items(a.B, a.Tq, a.Tk, a.H, RG);
+    HDT_CUDA_CHECK(launch_dependent(k_self_step<D, BF16, RG>, false, dim3((unsigned)(((long long)a.items * a.H + 3) / 4)), 128, 0, st, a));
+    if (a.Tk <= a.piece) return HDT_OK;      // no document of several pieces
+    HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)(((long long)a.Tq * a.H + 3) / 4)), 128, 0, st, a));
+    return HDT_OK;
+}
+template <int D, bool BF16>
+int step_rows(const StepArgs &a, cudaStream_t st) {
+    return step_group(a.B, a.Tq) == 1 ? step_go<D, BF16, 1>(a, st) : step_go<D, BF16, STEP_ROWS>(a, st);
+}
+
+struct Prepared { SelfLists q, k; SelfDist dist; };
+int prepare(const Layout &L, char *ws, const int32_t *cu_q, const int32_t *cu_k, const int32_t *len_k, int B, int Tq, int Tk, int H, int buckets, int max_distance,
+            int causal, const void *table, int dtype, int bwd, cudaStream_t st, Prepared *out) {
+    PrepArgs p{};
+    p.cu_q = cu_q; p.cu_k = cu_k; p.len_k = len_k; p.B = B; p.Tq = Tq; p.Tk = Tk; p.H = H;
+    p.n_lists = bwd ? 2 : 1;
+    int *count = (int *)(ws + L.count);
+    SelfBlk *raw = (SelfBlk *)(ws + L.raw);
+    p.list[0] = PrepList{raw, (SelfBlk *)(ws + L.q), count, L.rows_q, 0, L.most_q};
+    p.list[1] = PrepList{raw + L.most_q, (SelfBlk *)(ws + L.k), count + 1, dtype == HDT_F32 ? SELF_F32_ROWS : 128, 1, L.most_k};
+    p.rel.causal = causal;
+    p.dtype = dtype;
+    *out = Prepared{};
+    if (buckets > 0) {
+        rel_fill(&p.rel, buckets, max_distance, causal);
+        p.table = table;
+        p.lo = causal ? 0 : -p.rel.far;
+        p.n = p.rel.far - p.lo + 1;
+        p.bias = (float *)(ws + L.bias);
+        p.bucket = (unsigned char *)(ws + L.bucket);
+        out->dist = SelfDist{p.bias, p.bucket, p.lo, p.rel.far, p.n};
+    }
+    out->q = SelfLists{p.list[0].out, count, L.most_q};
+    out->k = SelfLists{p.list[1].out, count + 1, L.most_k};
+    HDT_CUDA_CHECK(launch_dependent(k_self_prep, false, dim3((unsigned)(p.n_lists + (p.n + 1023) / 1024)), 1024, 0, st, p));
+    return HDT_OK;
+}
+
+}  // namespace
+}  // namespace hdt
+
+using namespace hdt;
+
+extern "C" size_t hdt_self_workspace_bytes(int32_t batch, int32_t total_q, int32_t total_k, int32_t heads, int32_t head_dim, int32_t num_buckets,
+                                           int32_t max_distance, int32_t causal, int32_t dtype, int32_t bwd) {
+    if (sizes_check(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, "hdt_self_workspace_bytes")) return 0;
+    return layout(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal ? 1 : 0, dtype, bwd).total;
+}
+
+extern "C" int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch, int32_t total_q,
+                                 int32_t total_k, const void *q, const void *k, const void *v, const void *bias, int32_t num_buckets, int32_t max_distance,
+                                 int32_t causal, void *o, float *lse, int32_t heads, int32_t head_dim, int32_t dtype, float softmax_scale, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+    const char *who = "hdt_self_attn_fwd";
+    if (!bias) num_buckets = 0;
+    causal = causal ? 1 : 0;
+    if (const int rc = sizes_check(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, who)) return rc;
+    if (bias && num_buckets == 0) return set_error(HDT_ERR_INVALID_ARG, "%s: a bias without buckets", who);
+    const Layout L = layout(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, 0);
+    if (const int rc = ws_check(workspace, workspace_bytes, L.total, who)) return rc;
+    if (total_q == 0 || batch == 0) return HDT_OK;
+    if (!cu_seqlens_q || !cu_seqlens_k) return set_error(HDT_ERR_INVALID_ARG, "%s: null structure pointer", who);
+    if (total_k == 0) { if (!k) k = q; if (!v) v = q; }      // (never read)
+    for (const void *p : {q, k, v, (const void *)o})
+        if (const int rc = ptr_check(p, who)) return rc;
+    if (!lse || ((uintptr_t)lse & 3) || ((uintptr_t)bias & (dtype == HDT_F32 ? 3 : 1))) return set_error(HDT_ERR_INVALID_ARG, "%s: null or misaligned tensor", who);
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim), LOG2E = 1.4426950408889634f;
+    cudaStream_t st = (cudaStream_t)stream;
+    char *ws = (char *)workspace;
+    if (is_step(batch, total_q)) {
+        StepArgs s{};
+        s.cu_q = cu_seqlens_q; s.cu_k = cu_seqlens_k; s.len_k = seqlens_k; s.B = batch; s.Tq = total_q; s.Tk = total_k; s.H = heads;
+        s.piece = step_piece(total_k, heads); s.dtype = dtype;
+        s.q = q; s.k = k; s.v = v; s.table = bias; s.o = o; s.lse = lse; s.part_o = (float *)(ws + L.part_o); s.part_ml = (float *)(ws + L.part_ml);
+        s.scale_log2 = scale * LOG2E;
+        s.rel.causal = causal;
+        if (num_buckets > 0) rel_fill(&s.rel, num_buckets, max_distance, causal);
+        if (head_dim == 64) return dtype == HDT_BF16 ? step_rows<64, true>(s, st) : step_rows<64, false>(s, st);
+        return dtype == HDT_BF16 ? step_rows<128, true>(s, st) : step_rows<128, false>(s, st);
+    }
+    Prepared p;
+    if (const int rc = prepare(L, ws, cu_seqlens_q, cu_seqlens_k, seqlens_k, batch, total_q, total_k, heads, num_buckets, max_distance, causal, bias, dtype, 0, st, &p)) return rc;
+    SelfFwdArgs a{};
+    a.q = p.q; a.block_rows = L.rows_q; a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0;
+    a.qp = q; a.kp = k; a.vp = v; a.o = o; a.lse = lse; a.scale_log2 = scale * LOG2E;
+    a.status = device_status_ptr();
+    return dtype == HDT_BF16 ? launch_self_fwd_tc(a, head_dim, st) : launch_self_fwd_f32(a, head_dim, st);
+}
+
+extern "C" int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch, int32_t total_q,
+                                 int32_t total_k, const void *q, const void *k, const void *v, const void *bias, int32_t num_buckets, int32_t max_distance,
+                                 int32_t causal, const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *d_bias, int32_t heads,
+                                 int32_t head_dim, int32_t dtype, float softmax_scale, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *who = "hdt_self_attn_bwd";
+    if (!bias) num_buckets = 0;
+    causal = causal ? 1 : 0;
+    if (const int rc = sizes_check(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, who)) return rc;
+    if (bias && (num_buckets == 0 || !d_bias)) return set_error(HDT_ERR_INVALID_ARG, "%s: a bias without buckets or without room for its gradient", who);
+    const Layout L = layout(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, 1);
+    if (const int rc = ws_check(workspace, workspace_bytes, L.total, who)) return rc;
+    const uintptr_t el = dtype == HDT_F32 ? 3 : 1;
+    if (((uintptr_t)bias | (bias ? (uintptr_t)d_bias : 0)) & el) return set_error(HDT_ERR_INVALID_ARG, "%s: misaligned bias", who);
+    cudaStream_t st = (cudaStream_t)stream;
+    char *ws = (char *)workspace;
+    const bool none = batch == 0 || (total_q == 0 && total_k == 0);
+    Prepared p{};
+    if (!none) {
+        if (!cu_seqlens_q || !cu_seqlens_k) return set_error(HDT_ERR_INVALID_ARG, "%s: null structure pointer", who);
+        if (total_k == 0) { if (!k) k = q; if (!v) v = q; if (!dk) dk = dq; if (!dv) dv = dq; }      // (never read or written)
+        if (total_q == 0) { if (!q) q = k; if (!o) o = k; if (!d_o) d_o = k; if (!dq) dq = dk; if (!lse) lse = (const float *)k; }
+        for (const void *x : {q, k, v, o, d_o, (const void *)dq, (const void *)dk, (const void *)dv})
+            if (const int rc = ptr_check(x, who)) return rc;
+        if (!lse || ((uintptr_t)lse & 3)) return set_error(HDT_ERR_INVALID_ARG, "%s: null or misaligned tensor", who);
+        if (const int rc = prepare(L, ws, cu_seqlens_q, cu_seqlens_k, seqlens_k, batch, total_q, total_k, heads, num_buckets, max_distance, causal, bias, dtype, 1, st, &p)) return rc;
+        const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
+        SelfBwdArgs a{};
+        a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0; a.buckets = num_buckets;
+        a.qp = q; a.kp = k; a.vp = v; a.dop = d_o; a.lse = lse; a.delta = (const float *)(ws + L.delta); a.dq = dq; a.dk = dk; a.dv = dv;
+        a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.status = device_status_ptr();
+        if (const int rc = launch_delta(o, d_o, (float *)(ws + L.delta), total_q, heads, head_dim, dtype, st)) return rc;
+        SelfBwdArgs keys = a, rows = a;
+        keys.blk = p.k;
+        rows.blk = p.q;
+        rows.part = num_buckets > 0 ? (float *)(ws + L.part) : nullptr;
+        if (const int rc = dtype == HDT_BF16 ? launch_self_bwd_tc(keys, rows, head_dim, st) : launch_self_bwd_f32(keys, rows, head_dim, st)) return rc;
+    }
+    if (num_buckets > 0) {
+        const bool any = !none && total_q > 0;
+        HDT_CUDA_CHECK(launch_dependent(k_self_dbias, any, dim3((unsigned)heads), 1024, 0, st, any ? (const float *)(ws + L.part) : (const float *)nullptr, p.q.count, heads,
+                                        num_buckets, dtype, d_bias));
+    }
+    return HDT_OK;
+}

@@ -1,0 +1,297 @@
+// Self-attention with a relative position bias in fp32, forward and backward (there is no tcgen05 product of fp32
+// operands: the products run on the FMA pipe).  256 threads take 64 rows of one side, resident in shared memory, and walk
+// the other side in tiles of 64; a thread has a 4 x 4 piece of the tile (rows ty + 16 i, columns tx + 16 j, so that the 16-byte
+// reads of neighbouring threads lie in different banks) and 4 rows x D / 16 columns of a result (rows 4 ty + i, columns
+// 4 tx + 64 j).  A 64 x 64 product matrix goes from the one layout to the other through shared memory, transposed.
+// Bound by the shared-memory reads (two of 16 bytes for 16 fma).  Rows behind a document's end are stored as zeros.
+//
+// Forward: running maximum and sum of the softmax, O rescaled at every tile.  Backward as in bf16: once with keys resident
+// (dK, dV), once with rows resident (dQ, and the bias' gradient: the sums along the diagonals of the tile's dS, then by
+// bucket), no atomics.
+#include "hdt_self.cuh"
+
+namespace hdt {
+namespace {
+
+constexpr int R = SELF_F32_ROWS, PS = R + 4;      // row stride of a transposed 64 x 64 matrix
+template <int D>
+struct Shape { static constexpr int XS = D + 4, X = R * XS; };
+
+// 64 rows of [T, H, D] from `row` on, those behind `n` as zeros.
+template <int D>
+__device__ __forceinline__ void load_rows(float *dst, const float *src, int row, int n, int h, int H) {
+    for (int i = threadIdx.x; i < R * (D / 4); i += 256) {
+        const int r = i / (D / 4), c = 4 * (i % (D / 4));
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < n) x = *reinterpret_cast<const float4 *>(src + ((size_t)(row + r) * H + h) * D + c);
+        *reinterpret_cast<float4 *>(dst + r * Shape<D>::XS + c) = x;
+    }
+}
+// s[i][j] = a row (ty + 16 i) . b row (tx + 16 j)
+template <int D>
+__device__ __forceinline__ void dots(const float *a, const float *b, int ty, int tx, float (&s)[4][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < D; c += 4) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = *reinterpret_cast<const float4 *>(a + (ty + 16 * i) * Shape<D>::XS + c);
+            y[i] = *reinterpret_cast<const float4 *>(b + (tx + 16 * i) * Shape<D>::XS + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
+    }
+}
+// acc[i][..] += sum over columns c of p[c][4 ty + i] v[c][4 tx + 64 j ..]
+template <int D>
+__device__ __forceinline__ void accumulate(const float *p, const float *v, int ty, int tx, float (&acc)[4][D / 16]) {
+#pragma unroll 4
+    for (int c = 0; c < R; ++c) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + c * PS + 4 * ty);
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const float4 y = *reinterpret_cast<const float4 *>(v + c * Shape<D>::XS + 4 * tx + 64 * j);
+            const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                acc[i][4 * j] = fmaf(xs[i], y.x, acc[i][4 * j]);
+                acc[i][4 * j + 1] = fmaf(xs[i], y.y, acc[i][4 * j + 1]);
+                acc[i][4 * j + 2] = fmaf(xs[i], y.z, acc[i][4 * j + 2]);
+                acc[i][4 * j + 3] = fmaf(xs[i], y.w, acc[i][4 * j + 3]);
+            }
+        }
+    }
+}
+// bias' by distance of a tile: entry 63 + (distance - base)
+__device__ __forceinline__ void load_near(float *nb, const SelfDist &d, int h, int base) {
+    if (threadIdx.x < 2 * R) nb[threadIdx.x] = d.bias[(size_t)h * d.n + self_dist_at(d, base + (int)threadIdx.x - (R - 1))];
+}
+template <int D>
+__device__ __forceinline__ void store_rows(float *dst, const float (&acc)[4][D / 16], int row, int n, int h, int H, int ty, int tx) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (4 * ty + i < n)
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+                *reinterpret_cast<float4 *>(dst + ((size_t)(row + 4 * ty + i) * H + h) * D + 4 * tx + 64 * j) =
+                    make_float4(acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) k_self_fwd_f32(const SelfFwdArgs a) {
+    extern __shared__ float sm[];
+    float *sQ = sm, *sK = sQ + Shape<D>::X, *sV = sK + Shape<D>::X, *sP = sV + Shape<D>::X, *sF = sP + R * PS, *sNb = sF + R;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15, H = a.H;
+    pdl_wait();
+    const int n_units = *a.q.count * H;
+    for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
+        const SelfBlk b = a.q.blk[u / H];
+        const int h = u % H, rows = min(R, b.nq - b.r0), keys = self_keys_of(a.causal, b.r0, R, b.nq, b.nk);
+        __syncthreads();
+        load_rows<D>(sQ, (const float *)a.qp, b.q0 + b.r0, rows, h, H);
+        float acc[4][D / 16], m[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc[i][c] = 0.f;
+        }
+        for (int k = 0; k < keys; k += R) {
+            __syncthreads();
+            load_rows<D>(sK, (const float *)a.kp, b.k0 + k, b.nk - k, h, H);
+            load_rows<D>(sV, (const float *)a.vp, b.k0 + k, b.nk - k, h, H);
+            if (a.bias_on) load_near(sNb, a.dist, h, b.off + b.r0 - k);
+            __syncthreads();
+            float s[4][4];
+            dots<D>(sQ, sK, ty, tx, s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty + 16 * i, lim = a.causal ? b.off + b.r0 + r + 1 : b.nk;
+                float top = m[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = tx + 16 * j;
+                    s[i][j] = fmaf(s[i][j], a.scale_log2, a.bias_on ? sNb[R - 1 + r - c] : 0.f);
+                    if (k + c >= min(lim, b.nk)) s[i][j] = -INFINITY;
+                    top = fmaxf(top, s[i][j]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float use = top == -INFINITY ? 0.f : top, f = exp2f(m[i] - use);
+                m[i] = top;
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p = exp2f(s[i][j] - use);
+                    sum += p;
+                    sP[(tx + 16 * j) * PS + r] = p;
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                l[i] = l[i] * f + sum;
+                if (tx == 0) sF[r] = f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = sF[4 * ty + i];
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) acc[i][c] *= f;
+            }
+            accumulate<D>(sP, sV, ty, tx, acc);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (tx == 0) {
+                const int r = ty + 16 * i;
+                sF[r] = l[i] == 0.f ? 0.f : 1.f / l[i];
+                if (r < rows) a.lse[(size_t)h * a.Tq + b.q0 + b.r0 + r] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = sF[4 * ty + i];
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc[i][c] *= f;
+        }
+        store_rows<D>((float *)a.o, acc, b.q0 + b.r0, rows, h, H, ty, tx);
+    }
+}
+
+// ROWS: resident Q, dO, walked K, V: dQ and the sums of dS by bucket.  Else resident K, V, walked Q, dO: dK, dV.
+template <int D, bool ROWS>
+__global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
+    extern __shared__ float sm[];
+    float *sA = sm, *sB = sA + Shape<D>::X, *sX = sB + Shape<D>::X, *sY = sX + Shape<D>::X, *sP = sY + Shape<D>::X, *sD = sP + (ROWS ? 0 : R * PS);
+    float *sL = sD + R * PS, *sDel = sL + R, *sNb = sDel + R, *sDiag = sNb + 2 * R;
+    const int t = threadIdx.x, ty = t >> 4, tx = t & 15, H = a.H;
+    const float LOG2E = 1.4426950408889634f;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int n_units = *a.blk.count * H;
+    for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
+        const SelfBlk b = a.blk.blk[u / H];
+        const int h = u % H, rows = min(R, (ROWS ? b.nq : b.nk) - b.r0);
+        const int c0 = ROWS ? 0 : self_first_row(a.causal, b.r0, b.nq, b.nk), c1 = ROWS ? self_keys_of(a.causal, b.r0, R, b.nq, b.nk) : b.nq;
+        const int a0 = (ROWS ? b.q0 : b.k0) + b.r0, x0 = ROWS ? b.k0 : b.q0;
+        __syncthreads();
+        load_rows<D>(sA, (const float *)(ROWS ? a.qp : a.kp), a0, rows, h, H);
+        load_rows<D>(sB, (const float *)(ROWS ? a.dop : a.vp), a0, rows, h, H);
+        auto stats = [&](int row, int n) {      // LSE' and delta of 64 query rows
+            if (t >= R) return;
+            const size_t r = (size_t)h * a.Tq + row + t;
+            const float L = t < n ? a.lse[r] : -INFINITY;
+            sL[t] = L == -INFINITY ? INFINITY : L * LOG2E;
+            sDel[t] = t < n ? a.delta[r] : 0.f;
+        };
+        if (ROWS) stats(a0, rows);
+        float acc1[4][D / 16], acc2[4][ROWS ? 1 : D / 16], by_bucket = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc1[i][c] = 0.f;
+#pragma unroll
+            for (int c = 0; c < (ROWS ? 1 : D / 16); ++c) acc2[i][c] = 0.f;
+        }
+        for (int c = c0; c < c1; c += R) {
+            __syncthreads();
+            load_rows<D>(sX, (const float *)(ROWS ? a.kp : a.qp), x0 + c, c1 - c, h, H);
+            load_rows<D>(sY, (const float *)(ROWS ? a.vp : a.dop), x0 + c, c1 - c, h, H);
+            if (!ROWS) stats(x0 + c, c1 - c);
+            const int base = ROWS ? b.off + b.r0 - c : b.off + c - b.r0;      // distance of row 0 and column 0
+            if (a.bias_on) load_near(sNb, a.dist, h, base);
+            __syncthreads();
+            float s[4][4], d[4][4];
+            dots<D>(sA, sX, ty, tx, s);
+            dots<D>(sB, sY, ty, tx, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = ty + 16 * i, k = tx + 16 * j, q = ROWS ? r : k, step = ROWS ? r - k : k - r;
+                    const bool keep = r < rows && c + k < c1 && (!a.causal || base + step >= 0);
+                    const float y = fmaf(s[i][j], a.scale_log2, a.bias_on ? sNb[R - 1 + step] : 0.f) - sL[q];
+                    const float p = keep ? exp2f(y) : 0.f, ds = keep ? p * (d[i][j] - sDel[q]) : 0.f;
+                    if (!ROWS) sP[k * PS + r] = p;
+                    sD[k * PS + r] = ds;
+                }
+            __syncthreads();
+            accumulate<D>(sD, sX, ty, tx, acc1);
+            if constexpr (!ROWS) accumulate<D>(sP, sY, ty, tx, acc2);
+            if (ROWS && a.part != nullptr) {
+                if (t < 2 * R - 1) {      // the diagonal row - column = t - 63
+                    float v = 0.f;
+                    for (int r = max(0, t - (R - 1)); r < min(R, t + 1); ++r) v += sD[(r - (t - (R - 1))) * PS + r];
+                    sDiag[t] = v;
+                }
+                __syncthreads();
+                if (t < a.buckets)
+                    for (int i = 0; i < 2 * R - 1; ++i)
+                        if (a.dist.bucket[self_dist_at(a.dist, base + i - (R - 1))] == t) by_bucket += sDiag[i];
+            }
+        }
+        const float scale = a.scale;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) acc1[i][x] *= scale;
+        if constexpr (ROWS) {
+            store_rows<D>((float *)a.dq, acc1, a0, rows, h, H, ty, tx);
+            if (a.part != nullptr && t < a.buckets) a.part[((size_t)b.id * H + h) * a.buckets + t] = by_bucket;
+        } else {
+            store_rows<D>((float *)a.dk, acc1, a0, rows, h, H, ty, tx);
+            store_rows<D>((float *)a.dv, acc2, a0, rows, h, H, ty, tx);
+        }
+    }
+}
+
+template <int D>
+int fwd(const SelfFwdArgs &a, cudaStream_t st) {
+    constexpr int smem = (3 * Shape<D>::X + R * PS + R + 2 * R) * 4;
+    static DevOnce attr;
+    if (!attr.done()) {
+        HDT_CUDA_CHECK(cudaFuncSetAttribute(k_self_fwd_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        attr.set();
+    }
+    int n_sm = 0;
+    if (const int rc = sm_count(&n_sm)) return rc;
+    const long long units = (long long)a.q.most * a.H, most = 3LL * n_sm;
+    HDT_CUDA_CHECK(launch_dependent(k_self_fwd_f32<D>, true, dim3((unsigned)(units < most ? units : most)), 256, smem, st, a));
+    return HDT_OK;
+}
+template <int D, bool ROWS>
+int bwd(const SelfBwdArgs &a, cudaStream_t st) {
+    constexpr int smem = (4 * Shape<D>::X + (ROWS ? 1 : 2) * R * PS + 2 * R + 2 * R + 2 * R) * 4;
+    static DevOnce attr;
+    if (!attr.done()) {
+        HDT_CUDA_CHECK(cudaFuncSetAttribute(k_self_bwd_f32<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        attr.set();
+    }
+    int n_sm = 0;
+    if (const int rc = sm_count(&n_sm)) return rc;
+    const long long units = (long long)a.blk.most * a.H, most = 2LL * n_sm;
+    HDT_CUDA_CHECK(launch_dependent(k_self_bwd_f32<D, ROWS>, true, dim3((unsigned)(units < most ? units : most)), 256, smem, st, a));
+    return HDT_OK;
+}
+
+}  // namespace
+
+int launch_self_fwd_f32(const SelfFwdArgs &a, int head_dim, cudaStream_t st) { return head_dim == 64 ? fwd<64>(a, st) : fwd<128>(a, st); }
+int launch_self_bwd_f32(const SelfBwdArgs &keys, const SelfBwdArgs &rows, int head_dim, cudaStream_t st) {
+    if (keys.Tk > 0)
+        if (const int rc = head_dim == 64 ? bwd<64, false>(keys, st) : bwd<128, false>(keys, st)) return rc;
+    if (rows.Tq > 0)
+        if (const int rc = head_dim == 64 ? bwd<64, true>(rows, st) : bwd<128, true>(rows, st)) return rc;
+    return HDT_OK;
+}
+
+}  // namespace hdt

@@ -1,0 +1,594 @@
+// Self-attention with a relative position bias, backward in bf16 (TMA + tcgen05), head_dim 64 and 128: one kernel in
+// two forms, each with a block of 128 rows of one side in the TMEM lanes, which walks the other side in tiles of 128:
+//
+//   keys (dK, dV)   resident K, V; walked Q, dO:  S^T = K Q^T, dP^T = V dO^T;  dV += P^T dO, dK += dS^T Q
+//   rows (dQ)       resident Q, dO; walked K, V:  S = Q K^T, dP = dO V^T;      dQ += dS K
+//   P = exp2(S scale' + bias' - LSE'),   dS = scale P o (dP - delta)
+//
+// Both forms compute S and dP (seven products of a tile pair in all, one walk would need five), and in exchange nothing is
+// added up across CTAs: no fp32 buffer for dQ, no atomics, the same bits every run; and all four (three) tiles of a
+// product that the tensor pipe reads are where TMA or the compute warps put them, P and dS in TMEM.  That also is
+// what fits at head_dim 128, where dK and dV take half of TMEM.
+//
+// A unit is (block, head).  One CTA of 704 threads per SM walks units, dearest first:
+//   warps 0-7, 8-15   compute, 64 of a tile's columns each: a warp has a TMEM lane quarter and 32 columns
+//   warps 16-19       drain the accumulators at a unit's end: bf16 rows through a staging tile and TMA stores
+//   warp 20           requests the tiles (TMA); LSE and delta (keys) and the bias of the tile's distances
+//   warp 21           issues the MMAs
+// TMEM: S of the first 64 columns 0..63 (P over it), dP 64..127 (dS over it), of the second ones from 128;
+// accumulators from 256 (dK or dQ) and 256 + D (dV).
+//
+// Rows that are not the document's (the walked tile's tail) are set to zero in shared memory: their P and dS are 0, but
+// another document's rows, or unused ones, may hold NaN.
+//
+// The bias' gradient (rows form): the sum of dS over the pairs of a bucket.  In a tile whose distances are all beyond the
+// last border a thread adds its dS up in a register.  Elsewhere the sums run along the diagonals of a warp's 32 x 32
+// piece: column by column, each lane passes its sum to the next lane (one shuffle and one addition an entry),
+// so that a sum always stays with its distance; then neighbouring distances of one bucket are joined by a segmented
+// reduction.  All in fp32, from dS before its rounding, in an order that depends on nothing but the shapes.
+#include "hdt_self.cuh"
+#include "hdt_sm100.cuh"
+#include "hdt_tmap.cuh"
+
+namespace hdt {
+using namespace sm100;
+
+namespace {
+constexpr int SUB = 16384;                        // [128 rows x 64] bf16
+constexpr long long WAIT_CYCLES = 400000000LL;
+constexpr int KID = 10;                           // kernel id in the device status word
+__device__ __forceinline__ uint32_t swz(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+__device__ __forceinline__ bool group_all(bool pred, int id, int n) {      // barrier over a warp group: did all of them pass `pred`?
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, %2, %3, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)pred), "r"(id), "r"(n)
+        : "memory");
+    return r != 0;
+}
+
+template <int D, bool ROWS>
+struct BwdShape {
+    static constexpr int NS = D / 64, TILE = SUB * NS, RES = D == 64 ? 2 : 1, ST = D == 64 ? 3 : 2;
+    static constexpr int NACC = ROWS ? 1 : 2;
+    static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // LSE', delta by column; bias' and bucket by distance
+    static constexpr int SUMS = ROWS ? 16 * (SELF_MAX_BUCKETS + 32) * 4 : 0;
+    static constexpr int SMEM = (RES * 2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
+};
+}  // namespace
+
+template <int D, bool ROWS>
+__global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2,
+                                                     const __grid_constant__ CUtensorMap tm_s1, const __grid_constant__ CUtensorMap tm_s2,
+                                                     const __grid_constant__ StoreMaps sm_out, const SelfBwdArgs a) {
+    using Sh = BwdShape<D, ROWS>;
+    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST;
+    constexpr uint32_t TM_ACC = 256, TM_COLS = 512;
+    constexpr int W_DRAIN = 16, W_LOAD = 20, W_MMA = 21;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *sR = smem_raw;                       // [RES] x {R1, R2}: K, V or Q, dO
+    uint8_t *sS = sR + RES * 2 * TILE;            // [ST] x {S1, S2}: Q, dO or K, V
+    uint8_t *sStg = sS + ST * 2 * TILE;           // staging of 64 columns of a result
+    uint8_t *sStat = sStg + SUB;                  // [ST] x STAT
+    float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: per compute warp [buckets] and [32] of scratch
+    uint64_t *bars = (uint64_t *)((uint8_t *)sSum + Sh::SUMS);
+    uint64_t *r_full = bars, *r_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 7, *sdp_full = bars + 10, *pds_ready = bars + 12;
+    uint64_t *acc_full = bars + 14, *acc_free = bars + 15, *stat_full = bars + 16, *fix = bars + 19, *sum_full = bars + 20, *sum_free = bars + 21;
+    uint32_t *slot = (uint32_t *)(bars + 22);
+    volatile int *abort_flag = (volatile int *)(slot + 1);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.H;
+    const float LOG2E = 1.4426950408889634f;
+    if ((smem_u32(smem_raw) & 1023u) != 0u) {
+        if (tid == 0) atomicCAS(a.status, 0, HDT_ERR_CUDA);
+        return;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&r_full[i], 1);
+            mbar_init(&r_empty[i], 1);
+            mbar_init(&sdp_full[i], 1);
+            mbar_init(&pds_ready[i], 256);
+        }
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 1);
+            mbar_init(&stat_full[i], 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_free, 128);
+        mbar_init(fix, 1);
+        mbar_init(sum_full, 512);
+        mbar_init(sum_free, 128);
+        *abort_flag = (*a.status != 0);
+        fence_mbar_init();
+    }
+    if (ROWS)
+        for (int i = tid; i < Sh::SUMS / 4; i += 704) sSum[i] = 0.f;
+    if (warp == 0) tmem_alloc(slot, TM_COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *slot;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const bool dead = (*abort_flag != 0);
+    bool ok = true;
+    int fail_site = 0;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int n_units = *a.blk.count * H;
+    const bool sums = ROWS && a.part != nullptr;
+
+#define HDT_AGREE() (ok = __all_sync(0xffffffffu, ok))
+#define HDT_WAIT(bar, parity, site)                                                   \
+    do {                                                                              \
+        if (ok && !mbar_wait((bar), (uint32_t)(parity), abort_flag, WAIT_CYCLES)) {   \
+            ok = false;                                                               \
+            fail_site = (site);                                                       \
+        }                                                                             \
+    } while (0)
+
+    // What a unit walks: columns [c0, c1) of the other side (document numbers), in nt tiles.
+    struct Unit { SelfBlk b; int h, c0, c1, nt; };
+    auto unit = [&](int u) {
+        Unit x;
+        x.b = a.blk.blk[u / H];
+        x.h = u % H;
+        x.c0 = ROWS ? 0 : self_first_row(a.causal, x.b.r0, x.b.nq, x.b.nk);
+        x.c1 = ROWS ? self_keys_of(a.causal, x.b.r0, 128, x.b.nq, x.b.nk) : x.b.nq;
+        x.nt = (max(x.c1 - x.c0, 0) + 127) >> 7;
+        return x;
+    };
+    // Distance of lane 0 and column 0 of tile j; it grows by 1 per row and falls by 1 per key.
+    auto base_of = [&](const Unit &x, int j) { return ROWS ? x.b.off + x.b.r0 - 128 * j : x.b.off + x.c0 + 128 * j - x.b.r0; };
+    // -1, 1: all distances of the tile lie beyond the last border behind / before the query; 0: they do not
+    auto far_side = [&](int base) { return !a.bias_on ? 2 : base - 127 >= a.dist.far ? 1 : base + 127 <= -a.dist.far ? -1 : 0; };
+
+    if (!dead) {
+        if (warp == W_LOAD) {
+            // ================= load warp =================
+            int t = 0, uc = 0, nfix = 0;
+            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+                const Unit x = unit(u);
+                if (x.nt == 0) continue;
+                const int rb = uc % RES, rround = uc / RES;
+                if (rround > 0) HDT_WAIT(&r_empty[rb], (rround - 1) & 1, 1);
+                if (!HDT_AGREE()) break;
+                if (lane == 0) {
+                    const int row = (ROWS ? x.b.q0 : x.b.k0) + x.b.r0;
+                    uint8_t *d = sR + rb * 2 * TILE;
+                    mbar_expect_tx(&r_full[rb], 2u * TILE);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        tma_load_3d(d + s * SUB, &tm_r1, 64 * s, x.h, row, &r_full[rb]);
+                        tma_load_3d(d + TILE + s * SUB, &tm_r2, 64 * s, x.h, row, &r_full[rb]);
+                    }
+                }
+                ++uc;
+                const float *bias = a.dist.bias + (size_t)x.h * a.dist.n;
+                for (int j = 0; j < x.nt && ok; ++j, ++t) {
+                    const int s = t % ST, round = t / ST, col = x.c0 + 128 * j, rows = x.c1 - col, base = base_of(x, j), side = far_side(base);
+                    // into registers before the wait for the ring stage
+                    float2 st4[4];
+                    float nb[8];
+                    unsigned char bk[8];
+                    if (!ROWS) {
+                        const float c = side == 1 ? bias[a.dist.n - 1] : side == -1 ? bias[0] : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            st4[i] = make_float2(0.f, 0.f);
+                            if (lane + 32 * i < rows) {
+                                const size_t r = (size_t)x.h * a.Tq + x.b.q0 + col + lane + 32 * i;
+                                const float L = a.lse[r];
+                                // (a row without keys: every exponential is 0; one number for the tile's bias goes into the LSE)
+                                st4[i] = make_float2(L == -INFINITY ? INFINITY : L * LOG2E - c, a.delta[r] * a.scale);
+                            }
+                        }
+                    }
+                    if (side == 0) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int at = self_dist_at(a.dist, base + lane + 32 * i - 127);
+                            nb[i] = bias[at];
+                            bk[i] = sums ? a.dist.bucket[at] : 0;
+                        }
+                    }
+                    if (round > 0) HDT_WAIT(&s_empty[s], (round - 1) & 1, 2);
+                    if (!HDT_AGREE()) break;
+                    uint8_t *d = sS + s * 2 * TILE;
+                    uint64_t *bar = rows >= 128 ? &s_full[s] : fix;
+                    if (lane == 0) {
+                        const int row = (ROWS ? x.b.k0 : x.b.q0) + col;
+                        mbar_expect_tx(bar, 2u * TILE);
+#pragma unroll
+                        for (int c = 0; c < NS; ++c) {
+                            tma_load_3d(d + c * SUB, &tm_s1, 64 * c, x.h, row, bar);
+                            tma_load_3d(d + TILE + c * SUB, &tm_s2, 64 * c, x.h, row, bar);
+                        }
+                    }
+                    uint8_t *stat = sStat + s * Sh::STAT;
+                    if (!ROWS)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(stat)[lane + 32 * i] = st4[i];
+                    if (side == 0)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            reinterpret_cast<float *>(stat + 1024)[lane + 32 * i] = nb[i];
+                            stat[2048 + lane + 32 * i] = bk[i];
+                        }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&stat_full[s]);
+                    if (rows < 128) {
+                        HDT_WAIT(fix, nfix & 1, 3);
+                        ++nfix;
+                        if (!HDT_AGREE()) break;
+                        for (int i = lane; i < (128 - rows) * 8; i += 32)
+#pragma unroll
+                            for (int c = 0; c < 2 * NS; ++c) *reinterpret_cast<uint4 *>(d + c * SUB + rows * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&s_full[s]);
+                    }
+                }
+            }
+        } else if (warp == W_MMA) {
+            // ================= MMA warp =================
+            const uint32_t id_s = idesc_bf16(64, false, false), id_a = idesc_bf16(D, false, true);
+            const uint64_t d_r = smem_desc(smem_u32(sR), 0, 1024), d_sk = smem_desc(smem_u32(sS), 0, 1024), d_sm = smem_desc(smem_u32(sS), SUB, 1024);
+            const uint32_t r_hi = (uint32_t)(d_r >> 32), sk_hi = (uint32_t)(d_sk >> 32), sm_hi = (uint32_t)(d_sm >> 32);
+            constexpr uint32_t T16 = TILE >> 4, S16 = SUB >> 4;
+            auto issue_sdp = [&](int x, int s, int rb) {      // S and dP of columns 64 x ..
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t r_lo = (uint32_t)d_r + (rb * 2 + q) * T16, s_lo = (uint32_t)d_sk + (s * 2 + q) * T16 + x * (8192 >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        mma_ss_w(tmem + 128u * x + 64u * q, r_lo + (kk >> 2) * S16 + 2 * (kk & 3), r_hi, s_lo + (kk >> 2) * S16 + 2 * (kk & 3), sk_hi, id_s, kk > 0);
+                }
+                mma_commit(&sdp_full[x]);
+            };
+            auto issue_acc = [&](int x, int s, uint32_t acc) {      // columns 0..31 of the 64 packed in 16 TMEM columns, 32..63 from 32 on
+                const uint32_t b_lo = (uint32_t)d_sm + s * 2 * T16 + x * (8192 >> 4);
+                if (!ROWS)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_ts_w(tmem + TM_ACC + D, tmem + 128u * x + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + T16 + 128 * kk, sm_hi, id_a, acc | (kk > 0));
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_ts_w(tmem + TM_ACC, tmem + 128u * x + 64u + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
+            };
+            int t = 0, uc = 0, u = blockIdx.x, nt = 0;
+            auto next = [&]() {      // tiles of the next unit that has any
+                for (; u < n_units; u += gridDim.x) {
+                    const int n = unit(u).nt;
+                    if (n > 0) { u += gridDim.x; return n; }
+                }
+                return 0;
+            };
+            nt = next();
+            int nt_n = nt > 0 ? next() : 0, j = 0;
+            if (nt > 0) {
+                HDT_WAIT(&r_full[0], 0, 4);
+                HDT_WAIT(&s_full[0], 0, 5);
+                if (HDT_AGREE() && elect_one()) {
+                    tc_fence_after();
+                    issue_sdp(0, 0, 0);
+                    issue_sdp(1, 0, 0);
+                }
+                __syncwarp();
+            }
+            while (nt > 0 && ok) {
+                const int s = t % ST, s1 = (t + 1) % ST, rb = uc % RES;
+                const bool first = j == 0, last = j == nt - 1, more = !last || nt_n > 0;
+                const int uc1 = uc + (last ? 1 : 0);
+                if (first && uc > 0) HDT_WAIT(acc_free, (uc - 1) & 1, 6);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    HDT_WAIT(&pds_ready[x], t & 1, 7);
+                    if (!HDT_AGREE()) break;
+                    if (elect_one()) {
+                        tc_fence_after();
+                        issue_acc(x, s, first && x == 0 ? 0u : 1u);
+                        if (x == 1) {
+                            mma_commit(&s_empty[s]);      // (S and dP of this tile were issued before)
+                            if (last) mma_commit(acc_full);
+                        }
+                    }
+                    __syncwarp();
+                    if (more) {
+                        if (x == 0) {
+                            // (the resident buffer's last readers are S and dP of this tile's columns: complete, since P and dS are there)
+                            if (last && RES == 1) {
+                                HDT_WAIT(&pds_ready[1], t & 1, 8);      // those of the other half too
+                                if (!HDT_AGREE()) break;
+                                if (elect_one()) mma_commit(&r_empty[rb]);
+                                __syncwarp();
+                            }
+                            if (last) HDT_WAIT(&r_full[uc1 % RES], (uc1 / RES) & 1, 9);
+                            HDT_WAIT(&s_full[s1], ((t + 1) / ST) & 1, 10);
+                            if (!HDT_AGREE()) break;
+                        }
+                        if (elect_one()) {
+                            tc_fence_after();
+                            issue_sdp(x, s1, uc1 % RES);
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (!HDT_AGREE()) break;
+                if (last && RES > 1) {
+                    if (elect_one()) mma_commit(&r_empty[rb]);
+                    __syncwarp();
+                }
+                ++t;
+                if (!last) ++j;
+                else { nt = nt_n; nt_n = nt > 0 ? next() : 0; j = 0; ++uc; }
+            }
+        } else if (warp < W_DRAIN) {
+            // ================= compute: columns 64 x + 32 qh .. of every tile =================
+            const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane;
+            const uint32_t tm_s = tmem + 128u * x + 32u * qh + lane_base, tm_dp = tm_s + 64u;
+            float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;
+            int t = 0, uc = 0;
+            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+                const Unit U = unit(u);
+                if (U.nt == 0) {
+                    if (sums) {      // (the drain group writes the zeros)
+                        mbar_arrive(sum_full);
+                        HDT_WAIT(sum_free, uc & 1, 18);
+                        ++uc;
+                        if (!HDT_AGREE()) break;
+                    }
+                    continue;
+                }
+                const int row = U.b.r0 + rl;
+                const bool valid = row < (ROWS ? U.b.nq : U.b.nk);
+                float L = 0.f, delta = 0.f, far_sum[2] = {0.f, 0.f};
+                int first = 0, end = 0;      // columns that this lane's row pairs with
+                if (valid) {
+                    if (ROWS) {
+                        const size_t r = (size_t)U.h * a.Tq + U.b.q0 + row;
+                        L = a.lse[r];
+                        L = L == -INFINITY ? INFINITY : L * LOG2E;
+                        delta = a.delta[r] * a.scale;
+                        end = a.causal ? min(max(U.b.off + row + 1, 0), U.b.nk) : U.b.nk;
+                    } else {
+                        first = self_first_row(a.causal, row, U.b.nq, U.b.nk);
+                        end = U.b.nq;
+                    }
+                }
+                const float *bias = a.dist.bias + (size_t)U.h * a.dist.n;
+                for (int j = 0; j < U.nt; ++j, ++t) {
+                    const int s = t % ST, col = U.c0 + 128 * j + 64 * x + 32 * qh, side = far_side(base_of(U, j));
+                    const uint8_t *stat = sStat + s * Sh::STAT;
+                    const float c = ROWS && (side == 1 || side == -1) ? bias[side == 1 ? a.dist.n - 1 : 0] - L : -L;
+                    // entry (row, column) of a tile with near distances: + 1 per row, - 1 per key
+                    const float *nr = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - (64 * x + 32 * qh) : 64 * x + 32 * qh - rl);
+                    const int jl = max(first - col, 0), jh = min(end - col, 32);
+                    const uint32_t keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
+                    const bool any = __any_sync(0xffffffffu, keep != 0u), all = __all_sync(0xffffffffu, keep == 0xffffffffu);
+                    float diag = 0.f;
+                    HDT_WAIT(&stat_full[s], (t / ST) & 1, 11);
+                    HDT_WAIT(&sdp_full[x], t & 1, 12);
+                    if (!HDT_AGREE()) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t pp[8], pd[8];
+                        if (any) {
+                            uint32_t s_[16], d_[16];
+                            tmem_ld16(tm_s + 16u * i, s_);
+                            tmem_ld16(tm_dp + 16u * i, d_);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                float p[2], d[2];
+                                float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (!ROWS) st = *reinterpret_cast<const float4 *>(stat + 8 * (64 * x + 32 * qh + 16 * i + e));
+#pragma unroll
+                                for (int f = 0; f < 2; ++f) {
+                                    const int k = 16 * i + e + f;
+                                    const float c_ = ROWS ? c : -(f ? st.z : st.x), dl = ROWS ? delta : (f ? st.w : st.y);
+                                    float y = fmaf(__uint_as_float(s_[e + f]), a.scale_log2, c_);
+                                    if (side == 0) y += nr[ROWS ? -k : k];
+                                    p[f] = exp2f(y);
+                                    d[f] = p[f] * fmaf(__uint_as_float(d_[e + f]), a.scale, -dl);
+                                    if (!all && !(keep >> k & 1u)) p[f] = d[f] = 0.f;
+                                }
+                                if (!ROWS) pp[e >> 1] = pack_bf16(p[0], p[1]);
+                                pd[e >> 1] = pack_bf16(d[0], d[1]);
+                                if (ROWS && sums) {
+                                    if (side != 0) far_sum[side == -1] += d[0] + d[1];
+                                    else
+#pragma unroll
+                                        for (int f = 0; f < 2; ++f) {
+                                            const int k = 16 * i + e + f;
+                                            if (k > 0) {      // the sums move on by a lane; the last lane's is complete: distance 32 - k from lane 0 and column 0
+                                                diag = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
+                                                if (lane == 0) {
+                                                    scratch[k] = diag;
+                                                    diag = 0.f;
+                                                }
+                                            }
+                                            diag += d[f];
+                                        }
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) pp[e] = pd[e] = 0u;
+                        }
+                        if (!ROWS) tmem_st8(tm_s + 8u * i, pp);      // inside the columns that this warp alone reads
+                        tmem_st8(tm_dp + 8u * i, pd);
+                    }
+                    // distances lane - 31 (this lane's sum) and 32 - lane (in scratch, lanes 1..31) from the piece's corner: their
+                    // buckets, before the arrival that lets the load warp use the stage again
+                    int bks[2] = {255, 255};
+                    if (ROWS && sums && side == 0) {
+                        const uint8_t *at = stat + 2048 + 127 + (warp & 3) * 32 - (64 * x + 32 * qh);
+                        bks[0] = at[lane - 31];
+                        if (lane > 0) bks[1] = at[32 - lane];
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&pds_ready[x]);
+                    if (ROWS && sums && side == 0 && any) {
+                        __syncwarp();
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            const bool have = g == 0 || lane > 0;
+                            float v = g == 0 ? diag : have ? scratch[lane] : 0.f;
+                            const int bk = bks[g];
+#pragma unroll
+                            for (int o = 1; o < 32; o <<= 1) {      // sum of the lanes of one bucket from here on
+                                const float y = __shfl_down_sync(0xffffffffu, v, o);
+                                const int z = __shfl_down_sync(0xffffffffu, bk, o);
+                                if (lane + o < 32 && z == bk) v += y;
+                            }
+                            const int before = __shfl_up_sync(0xffffffffu, bk, 1);
+                            if (have && (lane == 0 || before != bk)) sum[bk] += v;
+                            __syncwarp();
+                        }
+                    }
+                }
+                if (!ok) break;
+                if (sums) {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) far_sum[g] += __shfl_xor_sync(0xffffffffu, far_sum[g], o);
+                    __syncwarp();
+                    if (lane == 0) {
+                        sum[a.dist.bucket[a.dist.n - 1]] += far_sum[0];
+                        if (!a.causal) sum[a.dist.bucket[0]] += far_sum[1];
+                    }
+                    mbar_arrive(sum_full);
+                    HDT_WAIT(sum_free, uc & 1, 18);      // (the drain group has read the sums and cleared them)
+                    if (!HDT_AGREE()) break;
+                }
+                ++uc;
+            }
+        } else if (warp < W_LOAD) {
+            // ================= drain group =================
+            const int rl = tid & 127;
+            int uc = 0, ua = 0;
+            for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
+                const Unit U = unit(u);
+                const int nrows = min(128, (ROWS ? U.b.nq : U.b.nk) - U.b.r0);
+                if (sums) {
+                    HDT_WAIT(sum_full, uc & 1, 13);
+                    if (HDT_AGREE() && rl < a.buckets) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int w = 0; w < 16; ++w) {
+                            float *p = sSum + w * (SELF_MAX_BUCKETS + 32) + rl;
+                            v += *p;
+                            *p = 0.f;
+                        }
+                        a.part[((size_t)U.b.id * H + U.h) * a.buckets + rl] = v / a.scale;
+                    }
+                    ++uc;
+                    if (ok) mbar_arrive(sum_free);
+                }
+                const int bx = max(__clz(nrows) - 25, 0), bbox = 64 >> bx;
+                if (U.nt > 0) {
+                    HDT_WAIT(acc_full, ua & 1, 14);
+                    ++ua;
+                }
+                bool go = group_all(ok, 1, 128);
+                if (!go) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < Sh::NACC * NS; ++c) {      // 64 columns of a result at a time
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t r[32];
+                        if (U.nt > 0) {
+                            tmem_ld32(tmem + TM_ACC + 64u * c + lane_base + 32u * half, r);
+                            tmem_wait_ld();
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) r[e] = 0u;
+                        }
+                        if (c == Sh::NACC * NS - 1 && half == 1 && U.nt > 0) {      // the accumulators have been read
+                            tc_fence_before();
+                            mbar_arrive(acc_free);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            *reinterpret_cast<uint4 *>(sStg + swz(rl, (32 * half + e) >> 3)) =
+                                make_uint4(pack_bf16(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pack_bf16(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])),
+                                           pack_bf16(__uint_as_float(r[e + 4]), __uint_as_float(r[e + 5])), pack_bf16(__uint_as_float(r[e + 6]), __uint_as_float(r[e + 7])));
+                    }
+                    fence_proxy_async_smem();
+                    group_all(true, 1, 128);
+                    // rows [0, nrows) as at most two boxes of b rows, b the largest power of two <= min(nrows, 64); where they
+                    // overlap the same values are written twice
+                    if (rl == 0) {
+                        const int which = ROWS ? 0 : 1 + c / NS, row = (ROWS ? U.b.q0 : U.b.k0) + U.b.r0;
+                        tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, row, sStg);
+                        if (nrows > bbox) tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, row + nrows - bbox, sStg + (nrows - bbox) * 128);
+                        bulk_commit();
+                        bulk_wait_read();
+                    }
+                    group_all(true, 1, 128);      // (the staging tile has been read)
+                }
+            }
+            if (rl == 0) bulk_wait_all();
+        }
+    }
+    if (!ok) {
+        if (atomicCAS(a.status, 0, HDT_ERR_TIMEOUT) == 0) {
+            a.status[1] = (KID << 8) | fail_site;
+            a.status[2] = (int)blockIdx.x;
+        }
+    }
+#undef HDT_WAIT
+#undef HDT_AGREE
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, TM_COLS);
+}
+
+template <int D, bool ROWS>
+static int go(const SelfBwdArgs &a, cudaStream_t st) {
+    static DevOnce attr;
+    using Sh = BwdShape<D, ROWS>;
+    if (!attr.done()) {
+        HDT_CUDA_CHECK(cudaFuncSetAttribute(k_self_bwd<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM));
+        attr.set();
+    }
+    int n_sm = 0;
+    if (const int rc = sm_count(&n_sm)) return rc;
+    CUtensorMap tq, tk, tv, tdo;
+    if (const int rc = make_tmap_bf16(&tq, a.qp, D, a.H, a.Tq, 128)) return rc;
+    if (const int rc = make_tmap_bf16(&tk, a.kp, D, a.H, a.Tk, 128)) return rc;
+    if (const int rc = make_tmap_bf16(&tv, a.vp, D, a.H, a.Tk, 128)) return rc;
+    if (const int rc = make_tmap_bf16(&tdo, a.dop, D, a.H, a.Tq, 128)) return rc;
+    StoreMaps outs;
+    void *const dst[3] = {a.dq, a.dk, a.dv};
+    for (int i = 0; i < 3; ++i) {
+        if (ROWS != (i == 0)) continue;
+        for (int b = 0; b < 7; ++b)
+            if (const int rc = make_tmap_bf16(&outs.m[i][b], dst[i], D, a.H, i == 0 ? a.Tq : a.Tk, 64 >> b)) return rc;
+    }
+    const long long units = (long long)a.blk.most * a.H;
+    const dim3 grid((unsigned)(units < n_sm ? units : n_sm));
+    if (ROWS) HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 704, Sh::SMEM, st, tq, tdo, tk, tv, outs, a));
+    else HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 704, Sh::SMEM, st, tk, tv, tq, tdo, outs, a));
+    return HDT_OK;
+}
+int launch_self_bwd_tc(const SelfBwdArgs &keys, const SelfBwdArgs &rows, int head_dim, cudaStream_t st) {
+    if (keys.Tk > 0)
+        if (const int rc = head_dim == 64 ? go<64, false>(keys, st) : go<128, false>(keys, st)) return rc;
+    if (rows.Tq > 0)
+        if (const int rc = head_dim == 64 ? go<64, true>(rows, st) : go<128, true>(rows, st)) return rc;
+    return HDT_OK;
+}
+
+}  // namespace hdt
