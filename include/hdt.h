@@ -368,7 +368,7 @@ int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const fl
  *   q, o, d_o, dq      device [total_q, heads, head_dim] of `dtype`, 16-byte aligned
  *   k, v, dk, dv       device [total_k, heads, head_dim]
  *   bias, d_bias       device [num_buckets, heads] of `dtype`; bias NULL: none (num_buckets, max_distance and d_bias
- *                      are not looked at).  Finite entries beyond +-30000 count as +-30000; -inf shuts a bucket out
+ *                      are not looked at).  Finite entries beyond +-32768 count as +-32768; -inf shuts a bucket out
  *   lse                device float [heads, total_q]
  *   workspace          device, >= hdt_self_workspace_bytes(..., bwd), 256-byte aligned; scratch.  num_buckets 0: no bias
  * 2 <= n, num_buckets <= 128 and even if not causal, n / 2 < max_distance <= 32768.  head_dim 64 or 128; softmax_scale <= 0
@@ -380,6 +380,8 @@ int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const fl
  * A call whose total_q is at most 4 x batch is taken as a step of autoregressive decoding (few rows a document, keys
  * split among warps).  Asynchronous on `stream`, no host wait; the offsets are read on the device only.
  */
+/* The buckets of one direction: first[b] = smallest distance of bucket b, for the n buckets.  Host arithmetic, no CUDA call. */
+int hdt_self_bucket_borders(int32_t num_buckets, int32_t max_distance, int32_t causal, int32_t *first);
 size_t hdt_self_workspace_bytes(int32_t batch, int32_t total_q, int32_t total_k, int32_t heads, int32_t head_dim,
                                 int32_t num_buckets, int32_t max_distance, int32_t causal, int32_t dtype, int32_t bwd);
 int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch,

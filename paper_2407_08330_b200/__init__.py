@@ -10,4 +10,4 @@ from .binding import (HdtError, HdtIndex, hdt_attn_bwd, hdt_attn_fwd, hdt_attn_w
                       hdt_device_status, hdt_attn_fwd_static, hdt_attn_fwd_static_max_bytes, hdt_hpe,
                       hdt_hpe_workspace_bytes, hdt_cross_attn_fwd, hdt_cross_attn_bwd, hdt_cross_workspace_bytes,
                       hdt_dropout, hdt_layer_norm_fwd, hdt_layer_norm_bwd, hdt_layer_norm_workspace_bytes,
-                      hdt_self_attn_fwd, hdt_self_attn_bwd, hdt_self_workspace_bytes)
+                      hdt_self_attn_fwd, hdt_self_attn_bwd, hdt_self_workspace_bytes, hdt_self_bucket_borders)

@@ -89,6 +89,8 @@ def lib():
         L.hdt_layer_norm_bwd.argtypes = [C.c_void_p] * 7 + [C.c_int32, C.c_float, C.c_int64] + [C.c_int32] * 3 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
         L.hdt_self_workspace_bytes.restype = C.c_size_t
         L.hdt_self_workspace_bytes.argtypes = [C.c_int32] * 10
+        L.hdt_self_bucket_borders.restype = C.c_int
+        L.hdt_self_bucket_borders.argtypes = [C.c_int32] * 3 + [C.POINTER(C.c_int32)]
         L.hdt_self_attn_fwd.restype = C.c_int
         L.hdt_self_attn_fwd.argtypes = [C.c_void_p] * 3 + [C.c_int32] * 3 + [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_void_p] * 2 + [C.c_int32] * 3 + \
                                        [C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -474,6 +476,13 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
 @functools.lru_cache(maxsize=256)
 def hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, bwd) -> int:
     return int(lib().hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, int(causal), _DTYPES[dtype], int(bwd)))
+
+
+def hdt_self_bucket_borders(num_buckets, max_distance, causal=True):
+    """Smallest distance of every bucket of one direction (a list of num_buckets, or of half of them if not causal)."""
+    first = (C.c_int32 * max(1, num_buckets))()
+    _check(lib().hdt_self_bucket_borders(int(num_buckets), int(max_distance), int(bool(causal)), first))
+    return list(first)[:num_buckets if causal else num_buckets // 2]
 
 
 def _self_common(cu_q, cu_k, seqlens_k, q, k, v, bias):

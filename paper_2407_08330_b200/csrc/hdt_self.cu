@@ -527,6 +527,15 @@ extern "C" size_t hdt_self_workspace_bytes(int32_t batch, int32_t total_q, int32
     return layout(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal ? 1 : 0, dtype, bwd).total;
 }
 
+extern "C" int hdt_self_bucket_borders(int32_t num_buckets, int32_t max_distance, int32_t causal, int32_t *first) {
+    if (num_buckets < 1 || !first) return set_error(HDT_ERR_INVALID_ARG, "hdt_self_bucket_borders: no bucket or a null pointer");
+    if (const int rc = sizes_check(0, 0, 0, 1, 64, num_buckets, max_distance, causal, HDT_F32, "hdt_self_bucket_borders")) return rc;
+    SelfRel r;
+    rel_fill(&r, num_buckets, max_distance, causal ? 1 : 0);
+    for (int b = 0; b < r.one_way; ++b) first[b] = r.first[b];
+    return HDT_OK;
+}
+
 extern "C" int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k, const int32_t *seqlens_k, int32_t batch, int32_t total_q,
                                  int32_t total_k, const void *q, const void *k, const void *v, const void *bias, int32_t num_buckets, int32_t max_distance,
                                  int32_t causal, void *o, float *lse, int32_t heads, int32_t head_dim, int32_t dtype, float softmax_scale, void *workspace,

@@ -15,7 +15,7 @@ namespace hdt {
 constexpr int SELF_MAX_BUCKETS = 128, SELF_MAX_DISTANCE = 32768;
 // A finite bias beyond this counts as this: fp32 logits of that size have lost the products they are added to, and
 // the difference of a logit and its row's LSE has to stay exact to a few thousandths.
-constexpr float SELF_MAX_BIAS = 30000.f;
+constexpr float SELF_MAX_BIAS = 32768.f;
 
 // Buckets of one direction: bucket b holds the distances [first[b], first[b + 1]).
 struct SelfRel {
