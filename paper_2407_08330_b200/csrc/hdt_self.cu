@@ -442,7 +442,7 @@ Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance
         }
         if (bwd) {
             L.delta = take((size_t)H * Tq * 4);
-            if (buckets > 0) L.part = take((size_t)L.most_q * H * buckets * 4);
+            if (buckets > 0) L.part = take((size_t)(dtype == HDT_F32 ? L.most_q : L.most_k) * H * buckets * 4);
         }
     }
     L.total = at > 0 ? at : 256;
@@ -604,18 +604,19 @@ extern "C" int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
         SelfBwdArgs a{};
         a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0; a.buckets = num_buckets;
-        a.qp = q; a.kp = k; a.vp = v; a.dop = d_o; a.lse = lse; a.delta = (const float *)(ws + L.delta); a.dq = dq; a.dk = dk; a.dv = dv;
+        a.qp = q; a.kp = k; a.vp = v; a.dop = d_o; a.lse = lse; a.delta = (float *)(ws + L.delta); a.dq = dq; a.dk = dk; a.dv = dv;
         a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.status = device_status_ptr();
         if (const int rc = launch_delta(o, d_o, (float *)(ws + L.delta), total_q, heads, head_dim, dtype, st)) return rc;
         SelfBwdArgs keys = a, rows = a;
         keys.blk = p.k;
         rows.blk = p.q;
-        rows.part = num_buckets > 0 ? (float *)(ws + L.part) : nullptr;
+        (dtype == HDT_F32 ? rows : keys).part = num_buckets > 0 ? (float *)(ws + L.part) : nullptr;
         if (const int rc = dtype == HDT_BF16 ? launch_self_bwd_tc(keys, rows, head_dim, st) : launch_self_bwd_f32(keys, rows, head_dim, st)) return rc;
     }
     if (num_buckets > 0) {
         const bool any = !none && total_q > 0;
-        HDT_CUDA_CHECK(launch_dependent(k_self_dbias, any, dim3((unsigned)heads), 1024, 0, st, any ? (const float *)(ws + L.part) : (const float *)nullptr, p.q.count, heads,
+        HDT_CUDA_CHECK(launch_dependent(k_self_dbias, any, dim3((unsigned)heads), 1024, 0, st, any ? (const float *)(ws + L.part) : (const float *)nullptr,
+                                        dtype == HDT_F32 ? p.q.count : p.k.count, heads,
                                         num_buckets, dtype, d_bias));
     }
     return HDT_OK;

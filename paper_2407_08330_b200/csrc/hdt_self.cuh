@@ -81,10 +81,11 @@ struct SelfBwdArgs {
     SelfDist dist;
     int H, Tq, Tk, causal, bias_on, buckets;
     const void *qp, *kp, *vp, *dop;
-    const float *lse, *delta;
+    const float *lse;
+    float *delta;            // rowsum(dO o O); bf16: put right by dQ's pass for that of dK and dV
     void *dq, *dk, *dv;
     float scale, scale_log2;
-    float *part;             // [block id][head][buckets]: sums of dS by bucket (dQ's pass), or nullptr
+    float *part;             // [block id][head][buckets]: sums of dS by bucket (the pass that is given it), or nullptr
     int *status;
 };
 int launch_self_fwd_tc(const SelfFwdArgs &a, int head_dim, cudaStream_t st);

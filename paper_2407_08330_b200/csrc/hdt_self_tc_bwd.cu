@@ -1,31 +1,38 @@
 // Self-attention with a relative position bias, backward in bf16 (TMA + tcgen05), head_dim 64 and 128: one kernel in
 // two forms, each with a block of 128 rows of one side in the TMEM lanes, which walks the other side in tiles of 128:
 //
-//   keys (dK, dV)   resident K, V; walked Q, dO:  S^T = K Q^T, dP^T = V dO^T;  dV += P^T dO, dK += dS^T Q
-//   rows (dQ)       resident Q, dO; walked K, V:  S = Q K^T, dP = dO V^T;      dQ += dS K
+//   rows (dQ), first   resident Q, dO; walked K, V:  S = Q K^T, dP = dO V^T;      dQ += dS K, W += P K
+//   keys (dK, dV)      resident K, V; walked Q, dO:  S^T = K Q^T, dP^T = V dO^T;  dK += dS^T Q, dV += P^T dO
 //   P = exp2(S scale' + bias' - LSE'),   dS = scale P o (dP - delta)
 //
-// Both forms compute S and dP (seven products of a tile pair in all, one walk would need five), and in exchange nothing is
-// added up across CTAs: no fp32 buffer for dQ, no atomics, the same bits every run; and all four (three) tiles of a
-// product that the tensor pipe reads are where TMA or the compute warps put them, P and dS in TMEM.  That also is
-// what fits at head_dim 128, where dK and dV take half of TMEM.
+// Both forms compute S and dP (eight products of a tile pair in all, one walk would need five), and in exchange nothing is
+// added up across CTAs: no fp32 buffer for dQ, no atomics, the same bits every run; and every operand that the tensor
+// pipe reads is where TMA or the compute warps put it, P and dS in TMEM.  That also is what fits at head_dim 128,
+// where two accumulators take half of TMEM.
+//
+// delta.  rowsum(dO o O) with the O that was rounded to bf16 is off by e = dO . (rounding of O), in every dS of the row by P e:
+// in rows of few keys as much as all other roundings together.  But the exact dS of a row add up to 0, so the row
+// sum of the computed ones, in fp32, IS -scale e.  The rows form takes it: dQ loses r W at the end (r the row sum, W = P K),
+// and delta is put right for the keys form.
 //
 // A unit is (block, head).  One CTA of 704 threads per SM walks units, dearest first:
-//   warps 0-7, 8-15   compute, 64 of a tile's columns each: a warp has a TMEM lane quarter and 32 columns
+//   warps 0-7, 8-15   compute, 64 of a tile's columns each (a step): a warp has a TMEM lane quarter and 32 columns
 //   warps 16-19       drain the accumulators at a unit's end: bf16 rows through a staging tile and TMA stores
 //   warp 20           requests the tiles (TMA); LSE and delta (keys) and the bias of the tile's distances
 //   warp 21           issues the MMAs
-// TMEM: S of the first 64 columns 0..63 (P over it), dP 64..127 (dS over it), of the second ones from 128;
-// accumulators from 256 (dK or dQ) and 256 + D (dV).
+// TMEM: step buffers of 128 columns, S 0..63 of it (P over it), dP 64..127 (dS over it), three at head_dim 64 and two at 128:
+// S and dP of a step are issued behind the products that read the buffer last, a step ahead of the compute
+// warps where there are three; the accumulators are the last 2 D columns.
 //
 // Rows that are not the document's (the walked tile's tail) are set to zero in shared memory: their P and dS are 0, but
 // another document's rows, or unused ones, may hold NaN.
 //
-// The bias' gradient (rows form): the sum of dS over the pairs of a bucket.  In a tile whose distances are all beyond the
+// The bias' gradient (keys form): the sum of dS over the pairs of a bucket.  In a tile whose distances are all beyond the
 // last border a thread adds its dS up in a register.  Elsewhere the sums run along the diagonals of a warp's 32 x 32
 // piece: column by column, each lane passes its sum to the next lane (one shuffle and one addition an entry),
 // so that a sum always stays with its distance; then neighbouring distances of one bucket are joined by a segmented
 // reduction.  All in fp32, from dS before its rounding, in an order that depends on nothing but the shapes.
+#include "hdt_rows.cuh"
 #include "hdt_self.cuh"
 #include "hdt_sm100.cuh"
 #include "hdt_tmap.cuh"
@@ -55,31 +62,65 @@ __device__ __forceinline__ bool group_all(bool pred, int id, int n) {      // ba
 template <int D, bool ROWS>
 struct BwdShape {
     static constexpr int NS = D / 64, TILE = SUB * NS, RES = D == 64 ? 2 : 1, ST = D == 64 ? 3 : 2;
-    static constexpr int NACC = ROWS ? 1 : 2;
-    static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // LSE', delta by column; bias' and bucket by distance
-    static constexpr int SUMS = ROWS ? 16 * (SELF_MAX_BUCKETS + 32) * 4 : 0;
+    static constexpr int NB = (512 - 2 * D) / 128;            // step buffers
+    static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // -LSE', -delta' by column; bias' and bucket by distance
+    static constexpr int SUMS = ROWS ? 4 * 128 * 4 : 16 * (SELF_MAX_BUCKETS + 32) * 4;
     static constexpr int SMEM = (RES * 2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
 };
 }  // namespace
+
+// 16 columns of a lane's row: P and dS from S and dP.  NEAR: a bias by distance (nr, step +-1 per column); MASK: only the columns of `keep`.
+template <bool ROWS, bool NEAR, bool MASK>
+__device__ __forceinline__ void piece(const uint32_t (&s_)[16], const uint32_t (&d_)[16], const float *neg_l, const float *neg_d, const float *nr, float row_l,
+                                      float row_d, float scale_log2, float scale, uint32_t keep, float (&p)[16], float (&d)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        f2 l[2], dl[2];
+        if constexpr (ROWS) {
+            l[0] = l[1] = pack2(row_l, row_l);
+            dl[0] = dl[1] = pack2(row_d, row_d);
+        } else {
+            const float4 x = *reinterpret_cast<const float4 *>(neg_l + e), y = *reinterpret_cast<const float4 *>(neg_d + e);
+            l[0] = pack2(x.x, x.y); l[1] = pack2(x.z, x.w);
+            dl[0] = pack2(y.x, y.y); dl[1] = pack2(y.z, y.w);
+        }
+#pragma unroll
+        for (int f = 0; f < 4; f += 2) {
+            const int k = e + f;
+            f2 y = fma2(pack2(__uint_as_float(s_[k]), __uint_as_float(s_[k + 1])), pack2(scale_log2, scale_log2), l[f >> 1]);
+            if constexpr (NEAR) y = add2(y, pack2(nr[ROWS ? -k : k], nr[ROWS ? -(k + 1) : k + 1]));
+            float y0, y1;
+            unpack2(y, y0, y1);
+            p[k] = exp2f(y0);
+            p[k + 1] = exp2f(y1);
+            const f2 g = mul2(pack2(p[k], p[k + 1]), fma2(pack2(__uint_as_float(d_[k]), __uint_as_float(d_[k + 1])), pack2(scale, scale), dl[f >> 1]));
+            unpack2(g, d[k], d[k + 1]);
+            if constexpr (MASK) {
+                if (!(keep >> k & 1u)) p[k] = d[k] = 0.f;
+                if (!(keep >> k & 2u)) p[k + 1] = d[k + 1] = 0.f;
+            }
+        }
+    }
+}
 
 template <int D, bool ROWS>
 __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2,
                                                      const __grid_constant__ CUtensorMap tm_s1, const __grid_constant__ CUtensorMap tm_s2,
                                                      const __grid_constant__ StoreMaps sm_out, const SelfBwdArgs a) {
     using Sh = BwdShape<D, ROWS>;
-    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST;
-    constexpr uint32_t TM_ACC = 256, TM_COLS = 512;
+    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST, NB = Sh::NB;
+    constexpr uint32_t TM_ACC = 512 - 2 * D, TM_COLS = 512;
     constexpr int W_DRAIN = 16, W_LOAD = 20, W_MMA = 21;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *sR = smem_raw;                       // [RES] x {R1, R2}: K, V or Q, dO
     uint8_t *sS = sR + RES * 2 * TILE;            // [ST] x {S1, S2}: Q, dO or K, V
     uint8_t *sStg = sS + ST * 2 * TILE;           // staging of 64 columns of a result
     uint8_t *sStat = sStg + SUB;                  // [ST] x STAT
-    float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: per compute warp [buckets] and [32] of scratch
+    float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: [4][128] row sums of dS; keys: per compute warp [buckets] and [32] of scratch
     uint64_t *bars = (uint64_t *)((uint8_t *)sSum + Sh::SUMS);
-    uint64_t *r_full = bars, *r_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 7, *sdp_full = bars + 10, *pds_ready = bars + 12;
-    uint64_t *acc_full = bars + 14, *acc_free = bars + 15, *stat_full = bars + 16, *fix = bars + 19, *sum_full = bars + 20, *sum_free = bars + 21;
-    uint32_t *slot = (uint32_t *)(bars + 22);
+    uint64_t *r_full = bars, *r_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 7, *sdp_full = bars + 10, *pds_ready = bars + 13;
+    uint64_t *acc_full = bars + 16, *acc_free = bars + 17, *stat_full = bars + 18, *fix = bars + 21, *sum_full = bars + 22, *sum_free = bars + 23;
+    uint32_t *slot = (uint32_t *)(bars + 24);
     volatile int *abort_flag = (volatile int *)(slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.H;
@@ -92,13 +133,13 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
         for (int i = 0; i < 2; ++i) {
             mbar_init(&r_full[i], 1);
             mbar_init(&r_empty[i], 1);
-            mbar_init(&sdp_full[i], 1);
-            mbar_init(&pds_ready[i], 256);
         }
         for (int i = 0; i < 3; ++i) {
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], 1);
             mbar_init(&stat_full[i], 1);
+            mbar_init(&sdp_full[i], 1);
+            mbar_init(&pds_ready[i], 256);
         }
         mbar_init(acc_full, 1);
         mbar_init(acc_free, 128);
@@ -108,8 +149,7 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
         *abort_flag = (*a.status != 0);
         fence_mbar_init();
     }
-    if (ROWS)
-        for (int i = tid; i < Sh::SUMS / 4; i += 704) sSum[i] = 0.f;
+    for (int i = tid; i < Sh::SUMS / 4; i += 704) sSum[i] = 0.f;
     if (warp == 0) tmem_alloc(slot, TM_COLS);
     tc_fence_before();
     __syncthreads();
@@ -122,7 +162,7 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
     pdl_wait();
     pdl_launch_dependents();
     const int n_units = *a.blk.count * H;
-    const bool sums = ROWS && a.part != nullptr;
+    const bool sums = !ROWS && a.part != nullptr;
 
 #define HDT_AGREE() (ok = __all_sync(0xffffffffu, ok))
 #define HDT_WAIT(bar, parity, site)                                                   \
@@ -174,19 +214,19 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                 for (int j = 0; j < x.nt && ok; ++j, ++t) {
                     const int s = t % ST, round = t / ST, col = x.c0 + 128 * j, rows = x.c1 - col, base = base_of(x, j), side = far_side(base);
                     // into registers before the wait for the ring stage
-                    float2 st4[4];
-                    float nb[8];
+                    float nl[4], nd[4], nb[8];
                     unsigned char bk[8];
                     if (!ROWS) {
                         const float c = side == 1 ? bias[a.dist.n - 1] : side == -1 ? bias[0] : 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            st4[i] = make_float2(0.f, 0.f);
+                            nl[i] = nd[i] = 0.f;
                             if (lane + 32 * i < rows) {
                                 const size_t r = (size_t)x.h * a.Tq + x.b.q0 + col + lane + 32 * i;
                                 const float L = a.lse[r];
                                 // (a row without keys: every exponential is 0; one number for the tile's bias goes into the LSE)
-                                st4[i] = make_float2(L == -INFINITY ? INFINITY : L * LOG2E - c, a.delta[r] * a.scale);
+                                nl[i] = L == -INFINITY ? -INFINITY : c - L * LOG2E;
+                                nd[i] = -a.delta[r] * a.scale;
                             }
                         }
                     }
@@ -214,7 +254,10 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                     uint8_t *stat = sStat + s * Sh::STAT;
                     if (!ROWS)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(stat)[lane + 32 * i] = st4[i];
+                        for (int i = 0; i < 4; ++i) {
+                            reinterpret_cast<float *>(stat)[lane + 32 * i] = nl[i];
+                            reinterpret_cast<float *>(stat)[128 + lane + 32 * i] = nd[i];
+                        }
                     if (side == 0)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -242,120 +285,96 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
             const uint64_t d_r = smem_desc(smem_u32(sR), 0, 1024), d_sk = smem_desc(smem_u32(sS), 0, 1024), d_sm = smem_desc(smem_u32(sS), SUB, 1024);
             const uint32_t r_hi = (uint32_t)(d_r >> 32), sk_hi = (uint32_t)(d_sk >> 32), sm_hi = (uint32_t)(d_sm >> 32);
             constexpr uint32_t T16 = TILE >> 4, S16 = SUB >> 4;
-            auto issue_sdp = [&](int x, int s, int rb) {      // S and dP of columns 64 x ..
+            auto issue_sdp = [&](int buf, int x, int s, int rb) {      // S and dP of columns 64 x ..
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const uint32_t r_lo = (uint32_t)d_r + (rb * 2 + q) * T16, s_lo = (uint32_t)d_sk + (s * 2 + q) * T16 + x * (8192 >> 4);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk)
-                        mma_ss_w(tmem + 128u * x + 64u * q, r_lo + (kk >> 2) * S16 + 2 * (kk & 3), r_hi, s_lo + (kk >> 2) * S16 + 2 * (kk & 3), sk_hi, id_s, kk > 0);
+                        mma_ss_w(tmem + 128u * buf + 64u * q, r_lo + (kk >> 2) * S16 + 2 * (kk & 3), r_hi, s_lo + (kk >> 2) * S16 + 2 * (kk & 3), sk_hi, id_s, kk > 0);
                 }
-                mma_commit(&sdp_full[x]);
+                mma_commit(&sdp_full[buf]);
             };
-            auto issue_acc = [&](int x, int s, uint32_t acc) {      // columns 0..31 of the 64 packed in 16 TMEM columns, 32..63 from 32 on
-                const uint32_t b_lo = (uint32_t)d_sm + s * 2 * T16 + x * (8192 >> 4);
-                if (!ROWS)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_ts_w(tmem + TM_ACC + D, tmem + 128u * x + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + T16 + 128 * kk, sm_hi, id_a, acc | (kk > 0));
+            auto issue_acc = [&](int buf, int x, int s, uint32_t acc) {      // columns 0..31 of the 64 packed in 16 TMEM columns, 32..63 from 32 on
+                const uint32_t b_lo = (uint32_t)d_sm + s * 2 * T16 + x * (8192 >> 4), p_lo = ROWS ? b_lo : b_lo + T16;
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
-                    mma_ts_w(tmem + TM_ACC, tmem + 128u * x + 64u + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
-            };
-            int t = 0, uc = 0, u = blockIdx.x, nt = 0;
-            auto next = [&]() {      // tiles of the next unit that has any
-                for (; u < n_units; u += gridDim.x) {
-                    const int n = unit(u).nt;
-                    if (n > 0) { u += gridDim.x; return n; }
-                }
-                return 0;
-            };
-            nt = next();
-            int nt_n = nt > 0 ? next() : 0, j = 0;
-            if (nt > 0) {
-                HDT_WAIT(&r_full[0], 0, 4);
-                HDT_WAIT(&s_full[0], 0, 5);
-                if (HDT_AGREE() && elect_one()) {
-                    tc_fence_after();
-                    issue_sdp(0, 0, 0);
-                    issue_sdp(1, 0, 0);
-                }
-                __syncwarp();
-            }
-            while (nt > 0 && ok) {
-                const int s = t % ST, s1 = (t + 1) % ST, rb = uc % RES;
-                const bool first = j == 0, last = j == nt - 1, more = !last || nt_n > 0;
-                const int uc1 = uc + (last ? 1 : 0);
-                if (first && uc > 0) HDT_WAIT(acc_free, (uc - 1) & 1, 6);
+                    mma_ts_w(tmem + TM_ACC + D, tmem + 128u * buf + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), p_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    HDT_WAIT(&pds_ready[x], t & 1, 7);
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_ts_w(tmem + TM_ACC, tmem + 128u * buf + 64u + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
+            };
+            // Two cursors over the steps of all units: `c` at the products with P and dS, `f` at S and dP, up to NB steps ahead.
+            struct Cursor { int u, nt, j, x, t, uc, buf, round; };      // u: next unit to look at; nt: tiles of this one, 0 behind the last
+            auto next_unit = [&](Cursor &k) {
+                k.nt = 0;
+                for (; k.u < n_units && k.nt == 0; k.u += gridDim.x) k.nt = unit(k.u).nt;
+                k.j = 0;
+            };
+            auto advance = [&](Cursor &k) {
+                if (++k.buf == NB) { k.buf = 0; k.round ^= 1; }
+                if (++k.x < 2) return;
+                k.x = 0;
+                ++k.t;
+                if (++k.j == k.nt) {
+                    ++k.uc;
+                    next_unit(k);
+                }
+            };
+            Cursor c{(int)blockIdx.x, 0, 0, 0, 0, 0, 0, 0};
+            next_unit(c);
+            Cursor f = c;
+            int ahead = 0;      // steps between the cursors
+            while (c.nt > 0 && ok) {
+                // (with one resident buffer the next unit's has to be loaded first: this unit's products go before the wait)
+                while (ahead < NB && f.nt > 0 && !(RES == 1 && f.uc > c.uc && ahead > 0)) {
+                    if (f.j == 0 && f.x == 0) HDT_WAIT(&r_full[f.uc % RES], (f.uc / RES) & 1, 4);
+                    if (f.x == 0) HDT_WAIT(&s_full[f.t % ST], (f.t / ST) & 1, 5);
                     if (!HDT_AGREE()) break;
                     if (elect_one()) {
                         tc_fence_after();
-                        issue_acc(x, s, first && x == 0 ? 0u : 1u);
-                        if (x == 1) {
-                            mma_commit(&s_empty[s]);      // (S and dP of this tile were issued before)
-                            if (last) mma_commit(acc_full);
-                        }
+                        issue_sdp(f.buf, f.x, f.t % ST, f.uc % RES);
+                        if (f.j == f.nt - 1 && f.x == 1) mma_commit(&r_empty[f.uc % RES]);      // the last that reads the resident tiles
                     }
                     __syncwarp();
-                    if (more) {
-                        if (x == 0) {
-                            // (the resident buffer's last readers are S and dP of this tile's columns: complete, since P and dS are there)
-                            if (last && RES == 1) {
-                                HDT_WAIT(&pds_ready[1], t & 1, 8);      // those of the other half too
-                                if (!HDT_AGREE()) break;
-                                if (elect_one()) mma_commit(&r_empty[rb]);
-                                __syncwarp();
-                            }
-                            if (last) HDT_WAIT(&r_full[uc1 % RES], (uc1 / RES) & 1, 9);
-                            HDT_WAIT(&s_full[s1], ((t + 1) / ST) & 1, 10);
-                            if (!HDT_AGREE()) break;
-                        }
-                        if (elect_one()) {
-                            tc_fence_after();
-                            issue_sdp(x, s1, uc1 % RES);
-                        }
-                        __syncwarp();
-                    }
+                    advance(f);
+                    ++ahead;
                 }
+                if (!ok) break;
+                if (c.j == 0 && c.x == 0 && c.uc > 0) HDT_WAIT(acc_free, (c.uc - 1) & 1, 6);
+                HDT_WAIT(&pds_ready[c.buf], c.round, 7);
                 if (!HDT_AGREE()) break;
-                if (last && RES > 1) {
-                    if (elect_one()) mma_commit(&r_empty[rb]);
-                    __syncwarp();
+                if (elect_one()) {
+                    tc_fence_after();
+                    issue_acc(c.buf, c.x, c.t % ST, c.j == 0 && c.x == 0 ? 0u : 1u);
+                    if (c.x == 1) {
+                        mma_commit(&s_empty[c.t % ST]);
+                        if (c.j == c.nt - 1) mma_commit(acc_full);
+                    }
                 }
-                ++t;
-                if (!last) ++j;
-                else { nt = nt_n; nt_n = nt > 0 ? next() : 0; j = 0; ++uc; }
+                __syncwarp();
+                advance(c);
+                --ahead;
             }
         } else if (warp < W_DRAIN) {
             // ================= compute: columns 64 x + 32 qh .. of every tile =================
-            const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane;
-            const uint32_t tm_s = tmem + 128u * x + 32u * qh + lane_base, tm_dp = tm_s + 64u;
-            float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;
-            int t = 0, uc = 0;
+            const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane, c0 = 64 * x + 32 * qh;
+            float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
+            int t = 0, uc = 0, buf = x, round = 0;
             for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 const Unit U = unit(u);
-                if (U.nt == 0) {
-                    if (sums) {      // (the drain group writes the zeros)
-                        mbar_arrive(sum_full);
-                        HDT_WAIT(sum_free, uc & 1, 18);
-                        ++uc;
-                        if (!HDT_AGREE()) break;
-                    }
-                    continue;
-                }
+                if (U.nt == 0) continue;
                 const int row = U.b.r0 + rl;
                 const bool valid = row < (ROWS ? U.b.nq : U.b.nk);
-                float L = 0.f, delta = 0.f, far_sum[2] = {0.f, 0.f};
+                float row_l = 0.f, row_d = 0.f, far_sum[2] = {0.f, 0.f};
+                f2 row_sum = pack2(0.f, 0.f);
                 int first = 0, end = 0;      // columns that this lane's row pairs with
                 if (valid) {
                     if (ROWS) {
                         const size_t r = (size_t)U.h * a.Tq + U.b.q0 + row;
-                        L = a.lse[r];
-                        L = L == -INFINITY ? INFINITY : L * LOG2E;
-                        delta = a.delta[r] * a.scale;
+                        const float L = a.lse[r];
+                        row_l = L == -INFINITY ? -INFINITY : -L * LOG2E;
+                        row_d = -a.delta[r] * a.scale;
                         end = a.causal ? min(max(U.b.off + row + 1, 0), U.b.nk) : U.b.nk;
                     } else {
                         first = self_first_row(a.causal, row, U.b.nq, U.b.nk);
@@ -364,17 +383,19 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                 }
                 const float *bias = a.dist.bias + (size_t)U.h * a.dist.n;
                 for (int j = 0; j < U.nt; ++j, ++t) {
-                    const int s = t % ST, col = U.c0 + 128 * j + 64 * x + 32 * qh, side = far_side(base_of(U, j));
+                    const int s = t % ST, col = U.c0 + 128 * j + c0, side = far_side(base_of(U, j));
                     const uint8_t *stat = sStat + s * Sh::STAT;
-                    const float c = ROWS && (side == 1 || side == -1) ? bias[side == 1 ? a.dist.n - 1 : 0] - L : -L;
+                    const uint32_t tm_s = tmem + 128u * buf + 32u * qh + lane_base, tm_dp = tm_s + 64u;
+                    const float l = ROWS && (side == 1 || side == -1) ? row_l + bias[side == 1 ? a.dist.n - 1 : 0] : row_l;
                     // entry (row, column) of a tile with near distances: + 1 per row, - 1 per key
-                    const float *nr = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - (64 * x + 32 * qh) : 64 * x + 32 * qh - rl);
+                    const float *nr = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - c0 : c0 - rl);
                     const int jl = max(first - col, 0), jh = min(end - col, 32);
                     const uint32_t keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
                     const bool any = __any_sync(0xffffffffu, keep != 0u), all = __all_sync(0xffffffffu, keep == 0xffffffffu);
                     float diag = 0.f;
+                    if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
                     HDT_WAIT(&stat_full[s], (t / ST) & 1, 11);
-                    HDT_WAIT(&sdp_full[x], t & 1, 12);
+                    HDT_WAIT(&sdp_full[buf], round, 12);
                     if (!HDT_AGREE()) break;
                     tc_fence_after();
 #pragma unroll
@@ -382,62 +403,66 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                         uint32_t pp[8], pd[8];
                         if (any) {
                             uint32_t s_[16], d_[16];
+                            float p[16], d[16];
                             tmem_ld16(tm_s + 16u * i, s_);
                             tmem_ld16(tm_dp + 16u * i, d_);
                             tmem_wait_ld();
+                            const float *neg_l = reinterpret_cast<const float *>(stat) + c0 + 16 * i, *neg_d = neg_l + 128, *n = nr + (ROWS ? -16 * i : 16 * i);
+                            const uint32_t k16 = keep >> (16 * i);
+                            if (side == 0) {
+                                if (all) piece<ROWS, true, false>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
+                                else piece<ROWS, true, true>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
+                            } else if (all) piece<ROWS, false, false>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
+                            else piece<ROWS, false, true>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) {
-                                float p[2], d[2];
-                                float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-                                if (!ROWS) st = *reinterpret_cast<const float4 *>(stat + 8 * (64 * x + 32 * qh + 16 * i + e));
+                                pp[e >> 1] = pack_bf16(p[e], p[e + 1]);
+                                pd[e >> 1] = pack_bf16(d[e], d[e + 1]);
+                                if (ROWS) row_sum = add2(row_sum, pack2(d[e], d[e + 1]));
+                            }
+                            if (sums && side != 0) {
+                                f2 v = pack2(0.f, 0.f);
 #pragma unroll
-                                for (int f = 0; f < 2; ++f) {
-                                    const int k = 16 * i + e + f;
-                                    const float c_ = ROWS ? c : -(f ? st.z : st.x), dl = ROWS ? delta : (f ? st.w : st.y);
-                                    float y = fmaf(__uint_as_float(s_[e + f]), a.scale_log2, c_);
-                                    if (side == 0) y += nr[ROWS ? -k : k];
-                                    p[f] = exp2f(y);
-                                    d[f] = p[f] * fmaf(__uint_as_float(d_[e + f]), a.scale, -dl);
-                                    if (!all && !(keep >> k & 1u)) p[f] = d[f] = 0.f;
-                                }
-                                if (!ROWS) pp[e >> 1] = pack_bf16(p[0], p[1]);
-                                pd[e >> 1] = pack_bf16(d[0], d[1]);
-                                if (ROWS && sums) {
-                                    if (side != 0) far_sum[side == -1] += d[0] + d[1];
-                                    else
+                                for (int e = 0; e < 16; e += 2) v = add2(v, pack2(d[e], d[e + 1]));
+                                float v0, v1;
+                                unpack2(v, v0, v1);
+                                far_sum[side == -1] += v0 + v1;
+                            } else if (sums) {
 #pragma unroll
-                                        for (int f = 0; f < 2; ++f) {
-                                            const int k = 16 * i + e + f;
-                                            if (k > 0) {      // the sums move on by a lane; the last lane's is complete: distance 32 - k from lane 0 and column 0
-                                                diag = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
-                                                if (lane == 0) {
-                                                    scratch[k] = diag;
-                                                    diag = 0.f;
-                                                }
-                                            }
-                                            diag += d[f];
+                                for (int e = 0; e < 16; ++e) {
+                                    // the sums move on by a lane; the last lane's is complete: distance k - 32 from lane 0 and column 0
+                                    const int k = 16 * i + e;
+                                    if (k > 0) {
+                                        diag = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
+                                        if (lane == 0) {
+                                            scratch[k] = diag;
+                                            diag = 0.f;
                                         }
+                                    }
+                                    diag += d[e];
                                 }
                             }
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; ++e) pp[e] = pd[e] = 0u;
                         }
-                        if (!ROWS) tmem_st8(tm_s + 8u * i, pp);      // inside the columns that this warp alone reads
+                        tmem_st8(tm_s + 8u * i, pp);      // inside the columns that this warp alone reads
                         tmem_st8(tm_dp + 8u * i, pd);
                     }
-                    // distances lane - 31 (this lane's sum) and 32 - lane (in scratch, lanes 1..31) from the piece's corner: their
+                    // distances 31 - lane (this lane's sum) and lane - 32 (in scratch, lanes 1..31) from the piece's corner: their
                     // buckets, before the arrival that lets the load warp use the stage again
                     int bks[2] = {255, 255};
-                    if (ROWS && sums && side == 0) {
-                        const uint8_t *at = stat + 2048 + 127 + (warp & 3) * 32 - (64 * x + 32 * qh);
-                        bks[0] = at[lane - 31];
-                        if (lane > 0) bks[1] = at[32 - lane];
+                    if (sums && side == 0) {
+                        const uint8_t *at = stat + 2048 + 127 + c0 - (warp & 3) * 32;
+                        bks[0] = at[31 - lane];
+                        if (lane > 0) bks[1] = at[lane - 32];
                     }
                     tmem_wait_st();
                     tc_fence_before();
-                    mbar_arrive(&pds_ready[x]);
-                    if (ROWS && sums && side == 0 && any) {
+                    mbar_arrive(&pds_ready[buf]);
+                    buf += 2;      // this group's next step
+                    if (buf >= NB) { buf -= NB; round ^= 1; }
+                    if (sums && side == 0 && any) {
                         __syncwarp();
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
@@ -457,7 +482,11 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                     }
                 }
                 if (!ok) break;
-                if (sums) {
+                if (ROWS) {
+                    float v0, v1;
+                    unpack2(row_sum, v0, v1);
+                    sSum[(2 * x + qh) * 128 + rl] = v0 + v1;
+                } else if (sums) {
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -467,72 +496,79 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                         sum[a.dist.bucket[a.dist.n - 1]] += far_sum[0];
                         if (!a.causal) sum[a.dist.bucket[0]] += far_sum[1];
                     }
-                    mbar_arrive(sum_full);
-                    HDT_WAIT(sum_free, uc & 1, 18);      // (the drain group has read the sums and cleared them)
-                    if (!HDT_AGREE()) break;
                 }
+                mbar_arrive(sum_full);
                 ++uc;
             }
         } else if (warp < W_LOAD) {
             // ================= drain group =================
             const int rl = tid & 127;
-            int uc = 0, ua = 0;
+            int uc = 0;
             for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
                 const Unit U = unit(u);
                 const int nrows = min(128, (ROWS ? U.b.nq : U.b.nk) - U.b.r0);
-                if (sums) {
-                    HDT_WAIT(sum_full, uc & 1, 13);
-                    if (HDT_AGREE() && rl < a.buckets) {
-                        float v = 0.f;
+                float r = 0.f;
+                if (U.nt > 0) HDT_WAIT(sum_full, uc & 1, 13);
+                if (HDT_AGREE()) {
+                    if (ROWS && U.nt > 0) {
 #pragma unroll
-                        for (int w = 0; w < 16; ++w) {
-                            float *p = sSum + w * (SELF_MAX_BUCKETS + 32) + rl;
-                            v += *p;
-                            *p = 0.f;
-                        }
+                        for (int w = 0; w < 4; ++w) r += sSum[w * 128 + rl];
+                        if (rl < nrows) a.delta[(size_t)U.h * a.Tq + U.b.q0 + U.b.r0 + rl] += r / a.scale;
+                    } else if (sums && rl < a.buckets) {
+                        float v = 0.f;
+                        if (U.nt > 0)
+#pragma unroll
+                            for (int w = 0; w < 16; ++w) {
+                                float *p = sSum + w * (SELF_MAX_BUCKETS + 32) + rl;
+                                v += *p;
+                                *p = 0.f;
+                            }
                         a.part[((size_t)U.b.id * H + U.h) * a.buckets + rl] = v / a.scale;
                     }
-                    ++uc;
-                    if (ok) mbar_arrive(sum_free);
+                    if (U.nt > 0) mbar_arrive(sum_free);
                 }
                 const int bx = max(__clz(nrows) - 25, 0), bbox = 64 >> bx;
                 if (U.nt > 0) {
-                    HDT_WAIT(acc_full, ua & 1, 14);
-                    ++ua;
+                    HDT_WAIT(acc_full, uc & 1, 14);
+                    ++uc;
                 }
                 bool go = group_all(ok, 1, 128);
                 if (!go) break;
                 tc_fence_after();
 #pragma unroll 1
-                for (int c = 0; c < Sh::NACC * NS; ++c) {      // 64 columns of a result at a time
+                for (int c = 0; c < (ROWS ? 1 : 2) * NS; ++c) {      // 64 columns of a result at a time
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint32_t r[32];
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t y[16], w[16];
                         if (U.nt > 0) {
-                            tmem_ld32(tmem + TM_ACC + 64u * c + lane_base + 32u * half, r);
+                            tmem_ld16(tmem + TM_ACC + 64u * c + lane_base + 16u * q, y);
+                            if (ROWS) tmem_ld16(tmem + TM_ACC + D + 64u * c + lane_base + 16u * q, w);
                             tmem_wait_ld();
+                            if (ROWS)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(fmaf(-r, __uint_as_float(w[e]), __uint_as_float(y[e])));
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) r[e] = 0u;
+                            for (int e = 0; e < 16; ++e) y[e] = 0u;
                         }
-                        if (c == Sh::NACC * NS - 1 && half == 1 && U.nt > 0) {      // the accumulators have been read
+                        if (c == (ROWS ? 1 : 2) * NS - 1 && q == 3 && U.nt > 0) {      // the accumulators have been read
                             tc_fence_before();
                             mbar_arrive(acc_free);
                         }
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4 *>(sStg + swz(rl, (32 * half + e) >> 3)) =
-                                make_uint4(pack_bf16(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pack_bf16(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])),
-                                           pack_bf16(__uint_as_float(r[e + 4]), __uint_as_float(r[e + 5])), pack_bf16(__uint_as_float(r[e + 6]), __uint_as_float(r[e + 7])));
+                        for (int e = 0; e < 16; e += 8)
+                            *reinterpret_cast<uint4 *>(sStg + swz(rl, (16 * q + e) >> 3)) =
+                                make_uint4(pack_bf16(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), pack_bf16(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3])),
+                                           pack_bf16(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5])), pack_bf16(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7])));
                     }
                     fence_proxy_async_smem();
                     group_all(true, 1, 128);
                     // rows [0, nrows) as at most two boxes of b rows, b the largest power of two <= min(nrows, 64); where they
                     // overlap the same values are written twice
                     if (rl == 0) {
-                        const int which = ROWS ? 0 : 1 + c / NS, row = (ROWS ? U.b.q0 : U.b.k0) + U.b.r0;
-                        tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, row, sStg);
-                        if (nrows > bbox) tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, row + nrows - bbox, sStg + (nrows - bbox) * 128);
+                        const int which = ROWS ? 0 : 1 + c / NS, at = (ROWS ? U.b.q0 : U.b.k0) + U.b.r0;
+                        tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, at, sStg);
+                        if (nrows > bbox) tma_store_3d(&sm_out.m[which][bx], 64 * (c % NS), U.h, at + nrows - bbox, sStg + (nrows - bbox) * 128);
                         bulk_commit();
                         bulk_wait_read();
                     }
@@ -584,10 +620,10 @@ static int go(const SelfBwdArgs &a, cudaStream_t st) {
     return HDT_OK;
 }
 int launch_self_bwd_tc(const SelfBwdArgs &keys, const SelfBwdArgs &rows, int head_dim, cudaStream_t st) {
-    if (keys.Tk > 0)
-        if (const int rc = head_dim == 64 ? go<64, false>(keys, st) : go<128, false>(keys, st)) return rc;
     if (rows.Tq > 0)
         if (const int rc = head_dim == 64 ? go<64, true>(rows, st) : go<128, true>(rows, st)) return rc;
+    if (keys.Tk > 0)
+        if (const int rc = head_dim == 64 ? go<64, false>(keys, st) : go<128, false>(keys, st)) return rc;
     return HDT_OK;
 }
 
