@@ -15,14 +15,19 @@
 // sum of the computed ones, in fp32, IS -scale e.  The rows form takes it: dQ loses r W at the end (r the row sum, W = P K),
 // and delta is put right for the keys form.
 //
-// A unit is (block, head).  One CTA of 704 threads per SM walks units, dearest first:
-//   warps 0-7, 8-15   compute, 64 of a tile's columns each (a step): a warp has a TMEM lane quarter and 32 columns
-//   warps 16-19       drain the accumulators at a unit's end: bf16 rows through a staging tile and TMA stores
+// A unit is (block, head).  One CTA of 768 threads per SM walks units, dearest first:
+//   warps 0-7, 8-15   compute, 64 of a tile's columns each (a step): a warp has a TMEM lane quarter and 32 columns, a thread
+//                     a lane; P from S, then dS from dP.  (Half the warps with 64 columns a thread: 2950 cycles a
+//                     step, whose exponentials take 512: two warps to a scheduler do not hide each other's latencies.)
+//   warps 16-19       bring the resident tiles from shared memory into TMEM (head_dim 64); drain the accumulators at a
+//                     unit's end: bf16 rows through a staging tile and TMA stores
 //   warp 20           requests the tiles (TMA); LSE and delta (keys) and the bias of the tile's distances
-//   warp 21           issues the MMAs
-// TMEM: step buffers of 128 columns, S 0..63 of it (P over it), dP 64..127 (dS over it), three at head_dim 64 and two at 128:
-// S and dP of a step are issued behind the products that read the buffer last, a step ahead of the compute
-// warps where there are three; the accumulators are the last 2 D columns.
+//   warp 21           issues the MMAs; warps 22 and 23 fill the warp group
+// What bounds it is the tensor pipe's operand reads: a product of M = 128, N = 64, K = 16 takes about 75 cycles with both
+// operands in shared memory and 40 with A in TMEM.  So at head_dim 64 the resident tiles lie in TMEM too.
+// TMEM at head_dim 64: S 3 x 64 columns (P over it), dP 2 x 64 (dS over it), accumulators 2 x 64, resident tiles 2 x 32; at 128:
+// S 2 x 64, dP 2 x 64, accumulators 2 x 128, resident tiles in shared memory.  A step's S is issued three (two) steps
+// ahead, behind the product that read P from the buffer, its dP two steps ahead behind the one that read dS.
 //
 // Rows that are not the document's (the walked tile's tail) are set to zero in shared memory: their P and dS are 0, but
 // another document's rows, or unused ones, may hold NaN.
@@ -61,55 +66,82 @@ __device__ __forceinline__ bool group_all(bool pred, int id, int n) {      // ba
 
 template <int D, bool ROWS>
 struct BwdShape {
-    static constexpr int NS = D / 64, TILE = SUB * NS, RES = D == 64 ? 2 : 1, ST = D == 64 ? 3 : 2;
-    static constexpr int NB = (512 - 2 * D) / 128;            // step buffers
+    static constexpr int NS = D / 64, TILE = SUB * NS, RES = 1, ST = D == 64 ? 4 : 2;
+    static constexpr bool RTM = D == 64;                      // the resident tiles are read from TMEM
+    static constexpr int NSB = D == 64 ? 3 : 2, NPB = 2;      // buffers of S and of dP
+    static constexpr uint32_t TM_S = 0, TM_P = 64 * NSB, TM_ACC = TM_P + 64 * NPB, TM_R = TM_ACC + 2 * D;
     static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // -LSE', -delta' by column; bias' and bucket by distance
     static constexpr int SUMS = ROWS ? 4 * 128 * 4 : 16 * (SELF_MAX_BUCKETS + 32) * 4;
     static constexpr int SMEM = (RES * 2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
 };
 }  // namespace
 
-// 16 columns of a lane's row: P and dS from S and dP.  NEAR: a bias by distance (nr, step +-1 per column); MASK: only the columns of `keep`.
+// P from S (in place, 32 columns of a lane's row), then dS from dP and P (in place, 16 columns at a time: with 32 the registers do not
+// hold them, and a spilled word is a trip to L2: 1500 cycles more a step).  NEAR: a bias by distance (nr, step +-1 per
+// column); MASK: only the columns of `keep`.
 template <bool ROWS, bool NEAR, bool MASK>
-__device__ __forceinline__ void piece(const uint32_t (&s_)[16], const uint32_t (&d_)[16], const float *neg_l, const float *neg_d, const float *nr, float row_l,
-                                      float row_d, float scale_log2, float scale, uint32_t keep, float (&p)[16], float (&d)[16]) {
+__device__ __forceinline__ void probabilities(uint32_t *x, const float *neg_l, const float *nr, float row_l, float scale_log2, uint32_t keep) {
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-        f2 l[2], dl[2];
-        if constexpr (ROWS) {
-            l[0] = l[1] = pack2(row_l, row_l);
-            dl[0] = dl[1] = pack2(row_d, row_d);
-        } else {
-            const float4 x = *reinterpret_cast<const float4 *>(neg_l + e), y = *reinterpret_cast<const float4 *>(neg_d + e);
-            l[0] = pack2(x.x, x.y); l[1] = pack2(x.z, x.w);
-            dl[0] = pack2(y.x, y.y); dl[1] = pack2(y.z, y.w);
+    for (int e = 0; e < 32; e += 4) {
+        f2 l[2] = {pack2(row_l, row_l), pack2(row_l, row_l)};
+        if constexpr (!ROWS) {
+            const float4 z = *reinterpret_cast<const float4 *>(neg_l + e);
+            l[0] = pack2(z.x, z.y);
+            l[1] = pack2(z.z, z.w);
         }
 #pragma unroll
         for (int f = 0; f < 4; f += 2) {
             const int k = e + f;
-            f2 y = fma2(pack2(__uint_as_float(s_[k]), __uint_as_float(s_[k + 1])), pack2(scale_log2, scale_log2), l[f >> 1]);
+            f2 y = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), pack2(scale_log2, scale_log2), l[f >> 1]);
             if constexpr (NEAR) y = add2(y, pack2(nr[ROWS ? -k : k], nr[ROWS ? -(k + 1) : k + 1]));
             float y0, y1;
             unpack2(y, y0, y1);
-            p[k] = exp2f(y0);
-            p[k + 1] = exp2f(y1);
-            const f2 g = mul2(pack2(p[k], p[k + 1]), fma2(pack2(__uint_as_float(d_[k]), __uint_as_float(d_[k + 1])), pack2(scale, scale), dl[f >> 1]));
-            unpack2(g, d[k], d[k + 1]);
+            y0 = exp2f(y0);
+            y1 = exp2f(y1);
             if constexpr (MASK) {
-                if (!(keep >> k & 1u)) p[k] = d[k] = 0.f;
-                if (!(keep >> k & 2u)) p[k + 1] = d[k + 1] = 0.f;
+                if (!(keep >> k & 1u)) y0 = 0.f;
+                if (!(keep >> k & 2u)) y1 = 0.f;
             }
+            x[k] = __float_as_uint(y0);
+            x[k + 1] = __float_as_uint(y1);
+        }
+    }
+}
+template <bool ROWS, bool MASK>
+__device__ __forceinline__ void gradients(uint32_t (&x)[16], const uint32_t *p, const float *neg_d, float row_d, float scale, uint32_t keep) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        f2 l[2] = {pack2(row_d, row_d), pack2(row_d, row_d)};
+        if constexpr (!ROWS) {
+            const float4 z = *reinterpret_cast<const float4 *>(neg_d + e);
+            l[0] = pack2(z.x, z.y);
+            l[1] = pack2(z.z, z.w);
+        }
+#pragma unroll
+        for (int f = 0; f < 4; f += 2) {
+            const int k = e + f;
+            const f2 g = mul2(pack2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])),
+                              fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), pack2(scale, scale), l[f >> 1]));
+            float y0, y1;
+            unpack2(g, y0, y1);
+            if constexpr (MASK) {      // (0 x NaN: a lane that is no row of the document may hold anything)
+                if (!(keep >> k & 1u)) y0 = 0.f;
+                if (!(keep >> k & 2u)) y1 = 0.f;
+            }
+            x[k] = __float_as_uint(y0);
+            x[k + 1] = __float_as_uint(y1);
         }
     }
 }
 
 template <int D, bool ROWS>
-__global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2,
+__global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2,
                                                      const __grid_constant__ CUtensorMap tm_s1, const __grid_constant__ CUtensorMap tm_s2,
                                                      const __grid_constant__ StoreMaps sm_out, const SelfBwdArgs a) {
     using Sh = BwdShape<D, ROWS>;
-    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST, NB = Sh::NB;
-    constexpr uint32_t TM_ACC = 512 - 2 * D, TM_COLS = 512;
+    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST, NSB = Sh::NSB, NPB = Sh::NPB;
+    constexpr uint32_t TM_S = Sh::TM_S, TM_P = Sh::TM_P, TM_ACC = Sh::TM_ACC, TM_R = Sh::TM_R, TM_COLS = 512;
+    constexpr bool RTM = Sh::RTM;
     constexpr int W_DRAIN = 16, W_LOAD = 20, W_MMA = 21;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *sR = smem_raw;                       // [RES] x {R1, R2}: K, V or Q, dO
@@ -118,9 +150,11 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
     uint8_t *sStat = sStg + SUB;                  // [ST] x STAT
     float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: [4][128] row sums of dS; keys: per compute warp [buckets] and [32] of scratch
     uint64_t *bars = (uint64_t *)((uint8_t *)sSum + Sh::SUMS);
-    uint64_t *r_full = bars, *r_empty = bars + 2, *s_full = bars + 4, *s_empty = bars + 7, *sdp_full = bars + 10, *pds_ready = bars + 13;
-    uint64_t *acc_full = bars + 16, *acc_free = bars + 17, *stat_full = bars + 18, *fix = bars + 21, *sum_full = bars + 22, *sum_free = bars + 23;
-    uint32_t *slot = (uint32_t *)(bars + 24);
+    // resident tiles: loaded, free, in TMEM, read for the last time; walked tiles; S, dP; P, dS; accumulators; the rest
+    uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 3, *s_full = bars + 4, *dp_full = bars + 7, *p_ready = bars + 9, *ds_ready = bars + 12;
+    uint64_t *acc_full = bars + 14, *acc_free = bars + 15, *fix = bars + 16, *sum_full = bars + 17, *sum_free = bars + 18;
+    uint64_t *t_full = bars + 19, *t_empty = t_full + ST, *stat_full = t_empty + ST;
+    uint32_t *slot = (uint32_t *)(stat_full + ST);
     volatile int *abort_flag = (volatile int *)(slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.H;
@@ -130,16 +164,22 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
         return;
     }
     if (tid == 0) {
+        mbar_init(r_full, 1);
+        mbar_init(r_empty, RTM ? 128 : 1);
+        mbar_init(r_ready, 128);
+        mbar_init(r_free, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&r_full[i], 1);
-            mbar_init(&r_empty[i], 1);
+            mbar_init(&dp_full[i], 1);
+            mbar_init(&ds_ready[i], 256);
         }
         for (int i = 0; i < 3; ++i) {
             mbar_init(&s_full[i], 1);
-            mbar_init(&s_empty[i], 1);
+            mbar_init(&p_ready[i], 256);
+        }
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&t_full[i], 1);
+            mbar_init(&t_empty[i], 1);
             mbar_init(&stat_full[i], 1);
-            mbar_init(&sdp_full[i], 1);
-            mbar_init(&pds_ready[i], 256);
         }
         mbar_init(acc_full, 1);
         mbar_init(acc_free, 128);
@@ -149,7 +189,7 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
         *abort_flag = (*a.status != 0);
         fence_mbar_init();
     }
-    for (int i = tid; i < Sh::SUMS / 4; i += 704) sSum[i] = 0.f;
+    for (int i = tid; i < Sh::SUMS / 4; i += 768) sSum[i] = 0.f;
     if (warp == 0) tmem_alloc(slot, TM_COLS);
     tc_fence_before();
     __syncthreads();
@@ -189,8 +229,193 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
     // -1, 1: all distances of the tile lie beyond the last border behind / before the query; 0: they do not
     auto far_side = [&](int base) { return !a.bias_on ? 2 : base - 127 >= a.dist.far ? 1 : base + 127 <= -a.dist.far ? -1 : 0; };
 
-    if (!dead) {
-        if (warp == W_LOAD) {
+    // 80 registers a thread at launch (768 threads): the compute warps take what the others do not need
+    // (512 x 88 + 256 x 64 = 768 x 80)
+    if (warp < W_DRAIN) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+        if (!dead) {
+            // ================= compute: columns c0 .. c0 + 31 of every tile =================
+            const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane, c0 = 64 * x + 32 * qh;
+            float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
+            const uint32_t tm_dp = tmem + TM_P + 64u * x + 32u * qh + lane_base;
+            int st = 0, tp = 0, uc = 0, sb = x, sr = 0, par = 0;
+            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+                // (what a unit needs in its loop, and no more: p and d fill the registers)
+                int nt, base, first, end;      // tiles; distance of lane 0 and column 0; columns that this lane's row pairs with, from c0 on
+                float row_l = 0.f, row_d = 0.f, by_side[2] = {0.f, 0.f};      // rows: -LSE' and -delta'; -LSE' with the bias of either side beyond the borders
+                {
+                    const Unit U = unit(u);
+                    if (U.nt == 0) continue;
+                    nt = U.nt;
+                    base = base_of(U, 0);
+                    const int row = U.b.r0 + rl;
+                    first = end = 0;
+                    if (row < (ROWS ? U.b.nq : U.b.nk)) {
+                        if (ROWS) {
+                            const size_t r = (size_t)U.h * a.Tq + U.b.q0 + row;
+                            const float L = a.lse[r];
+                            row_l = L == -INFINITY ? -INFINITY : -L * LOG2E;
+                            row_d = -a.delta[r] * a.scale;
+                            end = a.causal ? min(max(U.b.off + row + 1, 0), U.b.nk) : U.b.nk;
+                        } else {
+                            first = self_first_row(a.causal, row, U.b.nq, U.b.nk);
+                            end = U.b.nq;
+                        }
+                    }
+                    first -= U.c0 + c0;
+                    end -= U.c0 + c0;
+                    if (ROWS && a.bias_on) {
+                        by_side[0] = row_l + a.dist.bias[(size_t)U.h * a.dist.n];
+                        by_side[1] = row_l + a.dist.bias[(size_t)(U.h + 1) * a.dist.n - 1];
+                    }
+                }
+                float far_sum[2] = {0.f, 0.f};
+                f2 row_sum = pack2(0.f, 0.f);
+                for (int j = 0; j < nt; ++j) {
+                    const int side = far_side(base);
+                    base += ROWS ? -128 : 128;
+                    const uint8_t *stat = sStat + st * Sh::STAT;
+                    const uint32_t tm_s = tmem + TM_S + 64u * sb + 32u * qh + lane_base;
+                    const int jl = max(first, 0), jh = min(end, 32);
+                    first -= 128;
+                    end -= 128;
+                    const uint32_t keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
+                    const bool any = __any_sync(0xffffffffu, keep != 0u), all = __all_sync(0xffffffffu, keep == 0xffffffffu);
+                    const float l = !ROWS || side == 0 || side == 2 ? row_l : by_side[side == 1];
+                    if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
+                    HDT_WAIT(&stat_full[st], tp, 11);
+                    HDT_WAIT(&s_full[sb], sr, 12);
+                    if (!HDT_AGREE()) break;
+                    tc_fence_after();
+                    uint32_t p[32];
+                    if (any) {
+                        tmem_ld32(tm_s, p);
+                        tmem_wait_ld();
+                        const float *neg_l = reinterpret_cast<const float *>(stat) + c0;
+                        // entry (row, column) of a tile with near distances: + 1 per row, - 1 per key
+                        const float *n = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - c0 : c0 - rl);
+                        if (side == 0) {
+                            if (all) probabilities<ROWS, true, false>(p, neg_l, n, l, a.scale_log2, keep);
+                            else probabilities<ROWS, true, true>(p, neg_l, n, l, a.scale_log2, keep);
+                        } else if (all) probabilities<ROWS, false, false>(p, neg_l, n, l, a.scale_log2, keep);
+                        else probabilities<ROWS, false, true>(p, neg_l, n, l, a.scale_log2, keep);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) p[e] = 0u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = pack_bf16(__uint_as_float(p[16 * i + 2 * e]), __uint_as_float(p[16 * i + 2 * e + 1]));
+                        tmem_st8(tm_s + 8u * i, y);      // (inside the columns that this warp alone reads)
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&p_ready[sb]);
+                    HDT_WAIT(&dp_full[x], par, 15);
+                    if (!HDT_AGREE()) break;
+                    tc_fence_after();
+                    float diag = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t d[16], y[8];
+                        if (any) {
+                            tmem_ld16(tm_dp + 16u * i, d);
+                            tmem_wait_ld();
+                            const float *neg_d = reinterpret_cast<const float *>(stat) + 128 + c0 + 16 * i;
+                            if (all) gradients<ROWS, false>(d, p + 16 * i, neg_d, row_d, a.scale, 0u);
+                            else gradients<ROWS, true>(d, p + 16 * i, neg_d, row_d, a.scale, keep >> (16 * i));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) d[e] = 0u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = pack_bf16(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+                        tmem_st8(tm_dp + 8u * i, y);
+                        if (ROWS || (sums && side != 0)) {
+                            f2 v = pack2(0.f, 0.f);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) v = add2(v, pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])));
+                            if (ROWS) row_sum = add2(row_sum, v);
+                            else {
+                                float v0, v1;
+                                unpack2(v, v0, v1);
+                                far_sum[side == -1] += v0 + v1;
+                            }
+                        } else if (sums && any) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                // the sums move on by a lane; the last lane's is complete: distance k - 32 from lane 0 and column 0
+                                const int k = 16 * i + e;
+                                if (k > 0) {
+                                    diag = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
+                                    if (lane == 0) {
+                                        scratch[k] = diag;
+                                        diag = 0.f;
+                                    }
+                                }
+                                diag += __uint_as_float(d[e]);
+                            }
+                        }
+                    }
+                    // distances 31 - lane (this lane's sum) and lane - 32 (in scratch, lanes 1..31) from the piece's corner: their buckets,
+                    // before the arrival that lets the load warp use the stage again
+                    int bks[2] = {255, 255};
+                    if (sums && side == 0 && any) {
+                        const uint8_t *at = stat + 2048 + 127 + c0 - (warp & 3) * 32;
+                        bks[0] = at[31 - lane];
+                        if (lane > 0) bks[1] = at[lane - 32];
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&ds_ready[x]);
+                    if (++st == ST) { st = 0; tp ^= 1; }
+                    sb += 2;      // this group's next step
+                    if (sb >= NSB) { sb -= NSB; sr ^= 1; }
+                    par ^= 1;
+                    if (!(sums && side == 0 && any)) continue;
+                    __syncwarp();
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const bool have = g == 0 || lane > 0;
+                        float y = g == 0 ? diag : have ? scratch[lane] : 0.f;
+                        const int bk = bks[g];
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) {      // sum of the lanes of one bucket from here on
+                            const float y1 = __shfl_down_sync(0xffffffffu, y, o);
+                            const int z = __shfl_down_sync(0xffffffffu, bk, o);
+                            if (lane + o < 32 && z == bk) y += y1;
+                        }
+                        const int before = __shfl_up_sync(0xffffffffu, bk, 1);
+                        if (have && (lane == 0 || before != bk)) sum[bk] += y;
+                        __syncwarp();
+                    }
+                }
+                if (!ok) break;
+                if (ROWS) {
+                    float v0, v1;
+                    unpack2(row_sum, v0, v1);
+                    sSum[(2 * x + qh) * 128 + rl] = v0 + v1;
+                } else if (sums) {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) far_sum[g] += __shfl_xor_sync(0xffffffffu, far_sum[g], o);
+                    __syncwarp();
+                    if (lane == 0) {
+                        sum[a.dist.bucket[a.dist.n - 1]] += far_sum[0];
+                        if (!a.causal) sum[a.dist.bucket[0]] += far_sum[1];
+                    }
+                }
+                mbar_arrive(sum_full);
+                ++uc;
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (dead) {
+        } else if (warp == W_LOAD) {
             // ================= load warp =================
             int t = 0, uc = 0, nfix = 0;
             for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
@@ -238,10 +463,10 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                             bk[i] = sums ? a.dist.bucket[at] : 0;
                         }
                     }
-                    if (round > 0) HDT_WAIT(&s_empty[s], (round - 1) & 1, 2);
+                    if (round > 0) HDT_WAIT(&t_empty[s], (round - 1) & 1, 2);
                     if (!HDT_AGREE()) break;
                     uint8_t *d = sS + s * 2 * TILE;
-                    uint64_t *bar = rows >= 128 ? &s_full[s] : fix;
+                    uint64_t *bar = rows >= 128 ? &t_full[s] : fix;
                     if (lane == 0) {
                         const int row = (ROWS ? x.b.k0 : x.b.q0) + col;
                         mbar_expect_tx(bar, 2u * TILE);
@@ -275,237 +500,177 @@ __global__ void __launch_bounds__(704, 1) k_self_bwd(const __grid_constant__ CUt
                             for (int c = 0; c < 2 * NS; ++c) *reinterpret_cast<uint4 *>(d + c * SUB + rows * 128 + i * 16) = make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&s_full[s]);
+                        if (lane == 0) mbar_arrive(&t_full[s]);
                     }
                 }
             }
         } else if (warp == W_MMA) {
             // ================= MMA warp =================
-            const uint32_t id_s = idesc_bf16(64, false, false), id_a = idesc_bf16(D, false, true);
+            const uint32_t id_s = idesc_bf16(64, false, false), id_a = idesc_bf16(D, false, true), leader = elect_one() ? 1u : 0u;
             const uint64_t d_r = smem_desc(smem_u32(sR), 0, 1024), d_sk = smem_desc(smem_u32(sS), 0, 1024), d_sm = smem_desc(smem_u32(sS), SUB, 1024);
             const uint32_t r_hi = (uint32_t)(d_r >> 32), sk_hi = (uint32_t)(d_sk >> 32), sm_hi = (uint32_t)(d_sm >> 32);
             constexpr uint32_t T16 = TILE >> 4, S16 = SUB >> 4;
-            auto issue_sdp = [&](int buf, int x, int s, int rb) {      // S and dP of columns 64 x ..
+            // (TMEM is allocated whole, its addresses begin at 0)
+            auto issue_sdp = [&](uint32_t q, uint32_t dst, uint32_t x, uint32_t s) {      // S (q = 0) or dP (1) of columns 64 x ..
+                const uint32_t r_lo = (uint32_t)d_r + q * T16, s_lo = (uint32_t)d_sk + (s * 2u + q) * T16 + x * (8192u >> 4);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t r_lo = (uint32_t)d_r + (rb * 2 + q) * T16, s_lo = (uint32_t)d_sk + (s * 2 + q) * T16 + x * (8192 >> 4);
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        mma_ss_w(tmem + 128u * buf + 64u * q, r_lo + (kk >> 2) * S16 + 2 * (kk & 3), r_hi, s_lo + (kk >> 2) * S16 + 2 * (kk & 3), sk_hi, id_s, kk > 0);
-                }
-                mma_commit(&sdp_full[buf]);
-            };
-            auto issue_acc = [&](int buf, int x, int s, uint32_t acc) {      // columns 0..31 of the 64 packed in 16 TMEM columns, 32..63 from 32 on
-                const uint32_t b_lo = (uint32_t)d_sm + s * 2 * T16 + x * (8192 >> 4), p_lo = ROWS ? b_lo : b_lo + T16;
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_ts_w(tmem + TM_ACC + D, tmem + 128u * buf + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), p_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_ts_w(tmem + TM_ACC, tmem + 128u * buf + 64u + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + 128 * kk, sm_hi, id_a, acc | (kk > 0));
-            };
-            // Two cursors over the steps of all units: `c` at the products with P and dS, `f` at S and dP, up to NB steps ahead.
-            struct Cursor { int u, nt, j, x, t, uc, buf, round; };      // u: next unit to look at; nt: tiles of this one, 0 behind the last
-            auto next_unit = [&](Cursor &k) {
-                k.nt = 0;
-                for (; k.u < n_units && k.nt == 0; k.u += gridDim.x) k.nt = unit(k.u).nt;
-                k.j = 0;
-            };
-            auto advance = [&](Cursor &k) {
-                if (++k.buf == NB) { k.buf = 0; k.round ^= 1; }
-                if (++k.x < 2) return;
-                k.x = 0;
-                ++k.t;
-                if (++k.j == k.nt) {
-                    ++k.uc;
-                    next_unit(k);
+                for (uint32_t kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t o = (kk >> 2) * S16 + 2u * (kk & 3u);
+                    if (RTM) mma_ts_p(leader, dst, TM_R + 32u * q + 8u * kk, s_lo + o, sk_hi, id_s, kk > 0);
+                    else mma_ss_p(leader, dst, r_lo + o, r_hi, s_lo + o, sk_hi, id_s, kk > 0);
                 }
             };
-            Cursor c{(int)blockIdx.x, 0, 0, 0, 0, 0, 0, 0};
-            next_unit(c);
-            Cursor f = c;
-            int ahead = 0;      // steps between the cursors
-            while (c.nt > 0 && ok) {
-                // (with one resident buffer the next unit's has to be loaded first: this unit's products go before the wait)
-                while (ahead < NB && f.nt > 0 && !(RES == 1 && f.uc > c.uc && ahead > 0)) {
-                    if (f.j == 0 && f.x == 0) HDT_WAIT(&r_full[f.uc % RES], (f.uc / RES) & 1, 4);
-                    if (f.x == 0) HDT_WAIT(&s_full[f.t % ST], (f.t / ST) & 1, 5);
-                    if (!HDT_AGREE()) break;
-                    if (elect_one()) {
-                        tc_fence_after();
-                        issue_sdp(f.buf, f.x, f.t % ST, f.uc % RES);
-                        if (f.j == f.nt - 1 && f.x == 1) mma_commit(&r_empty[f.uc % RES]);      // the last that reads the resident tiles
-                    }
-                    __syncwarp();
-                    advance(f);
-                    ++ahead;
+            auto issue_acc = [&](uint32_t acc_at, uint32_t src, uint32_t q, uint32_t x, uint32_t s, uint32_t acc) {      // (columns 0..31 of P or dS in 16 of TMEM, 32..63 from 32 on)
+                const uint32_t b_lo = (uint32_t)d_sm + (s * 2u + q) * T16 + x * (8192u >> 4);
+#pragma unroll
+                for (uint32_t kk = 0; kk < 4; ++kk) mma_ts_p(leader, acc_at, src + (kk < 2 ? 8u * kk : 32u + 8u * (kk - 2)), b_lo + 128u * kk, sm_hi, id_a, acc | (kk > 0));
+            };
+            // Tile by tile: this one's products with P and dS, and between them S and dP of the tiles behind it.  What this warp
+            // keeps is counted: every instruction of it is on the critical chain.
+            int u_next = blockIdx.x;
+            auto next_nt = [&]() {      // tiles of the next unit that has any, 0 behind the last
+                int n = 0;
+                for (; u_next < n_units && n == 0; u_next += gridDim.x) n = __shfl_sync(0xffffffffu, unit(u_next).nt, 0);
+                return n;
+            };
+            auto wait = [&](uint64_t *bar, uint32_t parity, int site) {      // (the whole warp knows whether it ended well)
+                HDT_WAIT(bar, parity, site);
+                return HDT_AGREE();
+            };
+            int nt0 = next_nt(), nt1 = nt0 > 0 ? next_nt() : 0, nt2 = nt1 > 0 ? next_nt() : 0, j = 0;
+            uint32_t uc = 0, st = 0, tp = 0;     // unit; ring stage of this tile and parity of its use
+            uint32_t sb = 0, sp = 0, par = 0;    // S buffer of the tile's first step and parity of its use; parity of the tile number
+            auto tile_wait = [&](uint32_t k, bool opens, uint32_t unit_no) {      // the tile k behind this one is there, and its unit's resident tiles
+                if (opens && !wait(RTM ? r_ready : r_full, unit_no & 1u, 4)) return false;
+                const bool wrap = st + k >= ST;
+                return wait(&t_full[wrap ? st + k - ST : st + k], wrap ? tp ^ 1u : tp, 5);
+            };
+            auto put_s = [&](uint32_t step, uint32_t x, uint32_t k) {      // S of the step `step` behind the tile's first, columns 64 x .. of the tile k behind
+                const uint32_t b = sb + step, b1 = b >= 2 * NSB ? b - 2 * NSB : b >= NSB ? b - NSB : b, s_ = st + k >= ST ? st + k - ST : st + k;
+                tc_fence_after();
+                issue_sdp(0, TM_S + 64u * b1, x, s_);
+                mma_commit_p(leader, &s_full[b1]);
+            };
+            auto put_dp = [&](uint32_t x, uint32_t k, bool last_of_unit) {
+                issue_sdp(1, TM_P + 64u * x, x, st + k >= ST ? st + k - ST : st + k);
+                mma_commit_p(leader, &dp_full[x]);
+                if (last_of_unit && x == 1) mma_commit_p(leader, RTM ? r_free : r_empty);      // the last that reads the resident tiles
+            };
+            bool go = nt0 > 0 && tile_wait(0, true, 0);
+            if (go) {
+                put_s(0, 0, 0);
+                put_s(1, 1, 0);
+                put_dp(0, 0, false);
+                put_dp(1, 0, nt0 == 1);
+                if (NSB == 3 && (nt0 > 1 || nt1 > 0)) {
+                    go = tile_wait(1, nt0 == 1, 1);
+                    if (go) put_s(2, 0, 1);
                 }
-                if (!ok) break;
-                if (c.j == 0 && c.x == 0 && c.uc > 0) HDT_WAIT(acc_free, (c.uc - 1) & 1, 6);
-                HDT_WAIT(&pds_ready[c.buf], c.round, 7);
-                if (!HDT_AGREE()) break;
-                if (elect_one()) {
-                    tc_fence_after();
-                    issue_acc(c.buf, c.x, c.t % ST, c.j == 0 && c.x == 0 ? 0u : 1u);
-                    if (c.x == 1) {
-                        mma_commit(&s_empty[c.t % ST]);
-                        if (c.j == c.nt - 1) mma_commit(acc_full);
-                    }
-                }
-                __syncwarp();
-                advance(c);
-                --ahead;
             }
-        } else if (warp < W_DRAIN) {
-            // ================= compute: columns 64 x + 32 qh .. of every tile =================
-            const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane, c0 = 64 * x + 32 * qh;
-            float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
-            int t = 0, uc = 0, buf = x, round = 0;
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
-                const Unit U = unit(u);
-                if (U.nt == 0) continue;
-                const int row = U.b.r0 + rl;
-                const bool valid = row < (ROWS ? U.b.nq : U.b.nk);
-                float row_l = 0.f, row_d = 0.f, far_sum[2] = {0.f, 0.f};
-                f2 row_sum = pack2(0.f, 0.f);
-                int first = 0, end = 0;      // columns that this lane's row pairs with
-                if (valid) {
-                    if (ROWS) {
-                        const size_t r = (size_t)U.h * a.Tq + U.b.q0 + row;
-                        const float L = a.lse[r];
-                        row_l = L == -INFINITY ? -INFINITY : -L * LOG2E;
-                        row_d = -a.delta[r] * a.scale;
-                        end = a.causal ? min(max(U.b.off + row + 1, 0), U.b.nk) : U.b.nk;
-                    } else {
-                        first = self_first_row(a.causal, row, U.b.nq, U.b.nk);
-                        end = U.b.nq;
-                    }
-                }
-                const float *bias = a.dist.bias + (size_t)U.h * a.dist.n;
-                for (int j = 0; j < U.nt; ++j, ++t) {
-                    const int s = t % ST, col = U.c0 + 128 * j + c0, side = far_side(base_of(U, j));
-                    const uint8_t *stat = sStat + s * Sh::STAT;
-                    const uint32_t tm_s = tmem + 128u * buf + 32u * qh + lane_base, tm_dp = tm_s + 64u;
-                    const float l = ROWS && (side == 1 || side == -1) ? row_l + bias[side == 1 ? a.dist.n - 1 : 0] : row_l;
-                    // entry (row, column) of a tile with near distances: + 1 per row, - 1 per key
-                    const float *nr = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - c0 : c0 - rl);
-                    const int jl = max(first - col, 0), jh = min(end - col, 32);
-                    const uint32_t keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
-                    const bool any = __any_sync(0xffffffffu, keep != 0u), all = __all_sync(0xffffffffu, keep == 0xffffffffu);
-                    float diag = 0.f;
-                    if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
-                    HDT_WAIT(&stat_full[s], (t / ST) & 1, 11);
-                    HDT_WAIT(&sdp_full[buf], round, 12);
-                    if (!HDT_AGREE()) break;
+            while (go && nt0 > 0) {
+                const bool first = j == 0, last = j + 1 == nt0;
+                const bool more1 = !last || nt1 > 0, opens1 = last, last1 = last ? nt1 == 1 : j + 2 == nt0;      // the next tile
+                const bool more2 = more1 && (last1 ? (last ? nt2 : nt1) > 0 : true), opens2 = last1;              // the one behind it
+                // with one buffer of resident tiles in shared memory the next unit's come when this unit's last S and dP are through: its
+                // products go before the wait
+                const bool defer = !RTM && opens1;
+                if (first && uc > 0 && !wait(acc_free, (uc - 1) & 1u, 6)) break;
+#pragma unroll
+                for (uint32_t x = 0; x < 2; ++x) {
+                    const bool wrap = sb + x >= NSB;
+                    const uint32_t b = wrap ? sb + x - NSB : sb + x;
+                    go = wait(&p_ready[b], wrap ? sp ^ 1u : sp, 7);
+                    if (!go) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t pp[8], pd[8];
-                        if (any) {
-                            uint32_t s_[16], d_[16];
-                            float p[16], d[16];
-                            tmem_ld16(tm_s + 16u * i, s_);
-                            tmem_ld16(tm_dp + 16u * i, d_);
-                            tmem_wait_ld();
-                            const float *neg_l = reinterpret_cast<const float *>(stat) + c0 + 16 * i, *neg_d = neg_l + 128, *n = nr + (ROWS ? -16 * i : 16 * i);
-                            const uint32_t k16 = keep >> (16 * i);
-                            if (side == 0) {
-                                if (all) piece<ROWS, true, false>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
-                                else piece<ROWS, true, true>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
-                            } else if (all) piece<ROWS, false, false>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
-                            else piece<ROWS, false, true>(s_, d_, neg_l, neg_d, n, l, row_d, a.scale_log2, a.scale, k16, p, d);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                pp[e >> 1] = pack_bf16(p[e], p[e + 1]);
-                                pd[e >> 1] = pack_bf16(d[e], d[e + 1]);
-                                if (ROWS) row_sum = add2(row_sum, pack2(d[e], d[e + 1]));
-                            }
-                            if (sums && side != 0) {
-                                f2 v = pack2(0.f, 0.f);
-#pragma unroll
-                                for (int e = 0; e < 16; e += 2) v = add2(v, pack2(d[e], d[e + 1]));
-                                float v0, v1;
-                                unpack2(v, v0, v1);
-                                far_sum[side == -1] += v0 + v1;
-                            } else if (sums) {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    // the sums move on by a lane; the last lane's is complete: distance k - 32 from lane 0 and column 0
-                                    const int k = 16 * i + e;
-                                    if (k > 0) {
-                                        diag = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
-                                        if (lane == 0) {
-                                            scratch[k] = diag;
-                                            diag = 0.f;
-                                        }
-                                    }
-                                    diag += d[e];
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) pp[e] = pd[e] = 0u;
+                    issue_acc(TM_ACC + D, TM_S + 64u * b, ROWS ? 0 : 1, x, st, first && x == 0 ? 0u : 1u);
+                    if (NSB == 3) {      // S three steps ahead, into the buffer that P has just been read from
+                        if (x == 0) {
+                            if (more1) put_s(3, 1, 1);
+                        } else if (more2 && !opens2) {
+                            go = tile_wait(2, false, 0);
+                            if (!go) break;
+                            put_s(4, 0, 2);
                         }
-                        tmem_st8(tm_s + 8u * i, pp);      // inside the columns that this warp alone reads
-                        tmem_st8(tm_dp + 8u * i, pd);
-                    }
-                    // distances 31 - lane (this lane's sum) and lane - 32 (in scratch, lanes 1..31) from the piece's corner: their
-                    // buckets, before the arrival that lets the load warp use the stage again
-                    int bks[2] = {255, 255};
-                    if (sums && side == 0) {
-                        const uint8_t *at = stat + 2048 + 127 + c0 - (warp & 3) * 32;
-                        bks[0] = at[31 - lane];
-                        if (lane > 0) bks[1] = at[lane - 32];
-                    }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&pds_ready[buf]);
-                    buf += 2;      // this group's next step
-                    if (buf >= NB) { buf -= NB; round ^= 1; }
-                    if (sums && side == 0 && any) {
-                        __syncwarp();
-#pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            const bool have = g == 0 || lane > 0;
-                            float v = g == 0 ? diag : have ? scratch[lane] : 0.f;
-                            const int bk = bks[g];
-#pragma unroll
-                            for (int o = 1; o < 32; o <<= 1) {      // sum of the lanes of one bucket from here on
-                                const float y = __shfl_down_sync(0xffffffffu, v, o);
-                                const int z = __shfl_down_sync(0xffffffffu, bk, o);
-                                if (lane + o < 32 && z == bk) v += y;
-                            }
-                            const int before = __shfl_up_sync(0xffffffffu, bk, 1);
-                            if (have && (lane == 0 || before != bk)) sum[bk] += v;
-                            __syncwarp();
+                    } else if (more1 && !defer) {
+                        if (x == 0) {
+                            go = tile_wait(1, false, 0);
+                            if (!go) break;
                         }
+                        put_s(2 + x, x, 1);
                     }
-                }
-                if (!ok) break;
-                if (ROWS) {
-                    float v0, v1;
-                    unpack2(row_sum, v0, v1);
-                    sSum[(2 * x + qh) * 128 + rl] = v0 + v1;
-                } else if (sums) {
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) far_sum[g] += __shfl_xor_sync(0xffffffffu, far_sum[g], o);
-                    __syncwarp();
-                    if (lane == 0) {
-                        sum[a.dist.bucket[a.dist.n - 1]] += far_sum[0];
-                        if (!a.causal) sum[a.dist.bucket[0]] += far_sum[1];
+                    go = wait(&ds_ready[x], par, 8);
+                    if (!go) break;
+                    tc_fence_after();
+                    issue_acc(TM_ACC, TM_P + 64u * x, 0, x, st, first && x == 0 ? 0u : 1u);
+                    if (x == 1) {
+                        mma_commit_p(leader, &t_empty[st]);
+                        if (last) mma_commit_p(leader, acc_full);
                     }
+                    if (more1 && !defer) put_dp(x, 1, last1);
                 }
-                mbar_arrive(sum_full);
-                ++uc;
+                if (!go) break;
+                if (NSB == 3) {
+                    if (more2 && opens2) {      // (its resident tiles follow the last dP of the unit before it)
+                        go = tile_wait(2, true, uc + (last ? 2u : 1u));
+                        if (go) put_s(4, 0, 2);
+                    }
+                } else if (more1 && defer) {
+                    go = tile_wait(1, true, uc + 1);
+                    if (go)
+#pragma unroll
+                        for (uint32_t x = 0; x < 2; ++x) {
+                            put_s(2 + x, x, 1);
+                            put_dp(x, 1, last1);
+                        }
+                }
+                if (++st == ST) { st = 0; tp ^= 1u; }
+                sb += 2;
+                if (sb >= NSB) { sb -= NSB; sp ^= 1u; }
+                par ^= 1u;
+                ++j;
+                if (last) {
+                    nt0 = nt1; nt1 = nt2;
+                    nt2 = nt1 > 0 ? next_nt() : 0;
+                    j = 0;
+                    ++uc;
+                }
             }
         } else if (warp < W_LOAD) {
             // ================= drain group =================
             const int rl = tid & 127;
-            int uc = 0;
+            int uc = 0, um = 0, u_move = blockIdx.x;
+            // the resident tiles of the next unit that has any: from shared memory into TMEM, once the last products with those
+            // before them are through
+            auto move_next = [&]() {
+                if (!RTM) return;
+                for (; u_move < n_units && unit(u_move).nt == 0; u_move += gridDim.x) {}
+                if (u_move >= n_units) return;
+                u_move += gridDim.x;
+                const uint8_t *r = sR + (um % RES) * 2 * TILE;
+                HDT_WAIT(&r_full[um % RES], (um / RES) & 1, 16);
+                if (um > 0) HDT_WAIT(r_free, (um - 1) & 1, 17);
+                if (!HDT_AGREE()) return;
+                tc_fence_after();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {      // 32 columns of R1 or R2 at a time
+                    uint32_t y[16];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint4 z = *reinterpret_cast<const uint4 *>(r + (q >> 1) * TILE + swz(rl, 4 * (q & 1) + e));
+                        y[4 * e] = z.x; y[4 * e + 1] = z.y; y[4 * e + 2] = z.z; y[4 * e + 3] = z.w;
+                    }
+                    tmem_st16(tmem + TM_R + 16u * q + lane_base, y);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&r_empty[um % RES]);
+                mbar_arrive(r_ready);
+                ++um;
+            };
+            move_next();
             for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
                 const Unit U = unit(u);
+                if (U.nt > 0) move_next();
                 const int nrows = min(128, (ROWS ? U.b.nq : U.b.nk) - U.b.r0);
                 float r = 0.f;
                 if (U.nt > 0) HDT_WAIT(sum_full, uc & 1, 13);
@@ -615,8 +780,8 @@ static int go(const SelfBwdArgs &a, cudaStream_t st) {
     }
     const long long units = (long long)a.blk.most * a.H;
     const dim3 grid((unsigned)(units < n_sm ? units : n_sm));
-    if (ROWS) HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 704, Sh::SMEM, st, tq, tdo, tk, tv, outs, a));
-    else HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 704, Sh::SMEM, st, tk, tv, tq, tdo, outs, a));
+    if (ROWS) HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 768, Sh::SMEM, st, tq, tdo, tk, tv, outs, a));
+    else HDT_CUDA_CHECK(launch_dependent(k_self_bwd<D, ROWS>, true, grid, 768, Sh::SMEM, st, tk, tv, tq, tdo, outs, a));
     return HDT_OK;
 }
 int launch_self_bwd_tc(const SelfBwdArgs &keys, const SelfBwdArgs &rows, int head_dim, cudaStream_t st) {

@@ -213,6 +213,17 @@ def test_repeated_calls_give_the_same_bits(dtype, d):
     assert all(torch.equal(first[n], s.run(backward=False)[n]) for n in first)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_short_documents(dtype, d, causal):
+    """Several units of one tile, and of none, in a row for every CTA."""
+    lens = [(37 * i) % 150 for i in range(90)]
+    keys = [0 if i % 11 == 0 else n + (i % 3) * 40 for i, n in enumerate(lens)]
+    c = Case(lens, keys, 12, d, dtype, causal)
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("rows", [[300, 129], [1, 1]])
 def test_captured_and_replayed_with_other_lengths(rows):
     """Offsets are read on the device: one captured call serves whatever lengths the arrays hold at the replay."""
