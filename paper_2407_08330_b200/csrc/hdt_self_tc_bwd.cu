@@ -25,9 +25,9 @@
 //   warp 21           issues the MMAs; warps 22 and 23 fill the warp group
 // What bounds it is the tensor pipe's operand reads: a product of M = 128, N = 64, K = 16 takes about 75 cycles with both
 // operands in shared memory and 40 with A in TMEM.  So at head_dim 64 the resident tiles lie in TMEM too.
-// TMEM at head_dim 64: S 3 x 64 columns (P over it), dP 2 x 64 (dS over it), accumulators 2 x 64, resident tiles 2 x 32; at 128:
-// S 2 x 64, dP 2 x 64, accumulators 2 x 128, resident tiles in shared memory.  A step's S is issued three (two) steps
-// ahead, behind the product that read P from the buffer, its dP two steps ahead behind the one that read dS.
+// TMEM: S of either step 64 columns (P over it), dP 64 (dS over it), the accumulators 2 x 64 or 2 x 128, at head_dim 64 the
+// resident tiles 2 x 32.  One buffer of each is enough: S of a step's next tile is computed, behind the product that reads P,
+// while the compute warps are at dS, and dP, behind the one that reads dS, while they are at the next P.
 //
 // Rows that are not the document's (the walked tile's tail) are set to zero in shared memory: their P and dS are 0, but
 // another document's rows, or unused ones, may hold NaN.
@@ -68,8 +68,7 @@ template <int D, bool ROWS>
 struct BwdShape {
     static constexpr int NS = D / 64, TILE = SUB * NS, RES = 1, ST = D == 64 ? 4 : 2;
     static constexpr bool RTM = D == 64;                      // the resident tiles are read from TMEM
-    static constexpr int NSB = D == 64 ? 3 : 2, NPB = 2;      // buffers of S and of dP
-    static constexpr uint32_t TM_S = 0, TM_P = 64 * NSB, TM_ACC = TM_P + 64 * NPB, TM_R = TM_ACC + 2 * D;
+    static constexpr uint32_t TM_S = 0, TM_P = 128, TM_ACC = 256, TM_R = 384;
     static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // -LSE', -delta' by column; bias' and bucket by distance
     static constexpr int SUMS = ROWS ? 4 * 128 * 4 : 16 * (SELF_MAX_BUCKETS + 32) * 4;
     static constexpr int SMEM = (RES * 2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
@@ -139,7 +138,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                                                      const __grid_constant__ CUtensorMap tm_s1, const __grid_constant__ CUtensorMap tm_s2,
                                                      const __grid_constant__ StoreMaps sm_out, const SelfBwdArgs a) {
     using Sh = BwdShape<D, ROWS>;
-    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST, NSB = Sh::NSB, NPB = Sh::NPB;
+    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST;
     constexpr uint32_t TM_S = Sh::TM_S, TM_P = Sh::TM_P, TM_ACC = Sh::TM_ACC, TM_R = Sh::TM_R, TM_COLS = 512;
     constexpr bool RTM = Sh::RTM;
     constexpr int W_DRAIN = 16, W_LOAD = 20, W_MMA = 21;
@@ -151,9 +150,9 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
     float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: [4][128] row sums of dS; keys: per compute warp [buckets] and [32] of scratch
     uint64_t *bars = (uint64_t *)((uint8_t *)sSum + Sh::SUMS);
     // resident tiles: loaded, free, in TMEM, read for the last time; walked tiles; S, dP; P, dS; accumulators; the rest
-    uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 3, *s_full = bars + 4, *dp_full = bars + 7, *p_ready = bars + 9, *ds_ready = bars + 12;
-    uint64_t *acc_full = bars + 14, *acc_free = bars + 15, *fix = bars + 16, *sum_full = bars + 17, *sum_free = bars + 18;
-    uint64_t *t_full = bars + 19, *t_empty = t_full + ST, *stat_full = t_empty + ST;
+    uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 3, *s_full = bars + 4, *dp_full = bars + 6, *p_ready = bars + 8, *ds_ready = bars + 10;
+    uint64_t *acc_full = bars + 12, *acc_free = bars + 13, *fix = bars + 14, *sum_full = bars + 15, *sum_free = bars + 16;
+    uint64_t *t_full = bars + 17, *t_empty = t_full + ST, *stat_full = t_empty + ST;
     uint32_t *slot = (uint32_t *)(stat_full + ST);
     volatile int *abort_flag = (volatile int *)(slot + 1);
 
@@ -169,12 +168,10 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
         mbar_init(r_ready, 128);
         mbar_init(r_free, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&dp_full[i], 1);
-            mbar_init(&ds_ready[i], 256);
-        }
-        for (int i = 0; i < 3; ++i) {
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[i], 256);
+            mbar_init(&dp_full[i], 1);
+            mbar_init(&ds_ready[i], 256);
         }
         for (int i = 0; i < ST; ++i) {
             mbar_init(&t_full[i], 1);
@@ -237,8 +234,8 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             // ================= compute: columns c0 .. c0 + 31 of every tile =================
             const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane, c0 = 64 * x + 32 * qh;
             float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
-            const uint32_t tm_dp = tmem + TM_P + 64u * x + 32u * qh + lane_base;
-            int st = 0, tp = 0, uc = 0, sb = x, sr = 0, par = 0;
+            const uint32_t tm_s = tmem + TM_S + 64u * x + 32u * qh + lane_base, tm_dp = tmem + TM_P + 64u * x + 32u * qh + lane_base;
+            int st = 0, tp = 0, uc = 0, par = 0;
             for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 // (what a unit needs in its loop, and no more: p and d fill the registers)
                 int nt, base, first, end;      // tiles; distance of lane 0 and column 0; columns that this lane's row pairs with, from c0 on
@@ -275,7 +272,6 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     const int side = far_side(base);
                     base += ROWS ? -128 : 128;
                     const uint8_t *stat = sStat + st * Sh::STAT;
-                    const uint32_t tm_s = tmem + TM_S + 64u * sb + 32u * qh + lane_base;
                     const int jl = max(first, 0), jh = min(end, 32);
                     first -= 128;
                     end -= 128;
@@ -284,7 +280,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     const float l = !ROWS || side == 0 || side == 2 ? row_l : by_side[side == 1];
                     if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
                     HDT_WAIT(&stat_full[st], tp, 11);
-                    HDT_WAIT(&s_full[sb], sr, 12);
+                    HDT_WAIT(&s_full[x], par, 12);
                     if (!HDT_AGREE()) break;
                     tc_fence_after();
                     uint32_t p[32];
@@ -312,7 +308,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     }
                     tmem_wait_st();
                     tc_fence_before();
-                    mbar_arrive(&p_ready[sb]);
+                    mbar_arrive(&p_ready[x]);
                     HDT_WAIT(&dp_full[x], par, 15);
                     if (!HDT_AGREE()) break;
                     tc_fence_after();
@@ -371,8 +367,6 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     tc_fence_before();
                     mbar_arrive(&ds_ready[x]);
                     if (++st == ST) { st = 0; tp ^= 1; }
-                    sb += 2;      // this group's next step
-                    if (sb >= NSB) { sb -= NSB; sr ^= 1; }
                     par ^= 1;
                     if (!(sums && side == 0 && any)) continue;
                     __syncwarp();
@@ -438,22 +432,17 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                 const float *bias = a.dist.bias + (size_t)x.h * a.dist.n;
                 for (int j = 0; j < x.nt && ok; ++j, ++t) {
                     const int s = t % ST, round = t / ST, col = x.c0 + 128 * j, rows = x.c1 - col, base = base_of(x, j), side = far_side(base);
-                    // into registers before the wait for the ring stage
-                    float nl[4], nd[4], nb[8];
+                    // requested before the wait for the ring stage, all at once, and not looked at before the tile is
+                    float L[4], dl[4], c = 0.f, nb[8];
                     unsigned char bk[8];
                     if (!ROWS) {
-                        const float c = side == 1 ? bias[a.dist.n - 1] : side == -1 ? bias[0] : 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            nl[i] = nd[i] = 0.f;
-                            if (lane + 32 * i < rows) {
-                                const size_t r = (size_t)x.h * a.Tq + x.b.q0 + col + lane + 32 * i;
-                                const float L = a.lse[r];
-                                // (a row without keys: every exponential is 0; one number for the tile's bias goes into the LSE)
-                                nl[i] = L == -INFINITY ? -INFINITY : c - L * LOG2E;
-                                nd[i] = -a.delta[r] * a.scale;
-                            }
+                            const size_t r = (size_t)x.h * a.Tq + x.b.q0 + col + min(lane + 32 * i, rows - 1);
+                            L[i] = a.lse[r];
+                            dl[i] = a.delta[r];
                         }
+                        if (side == 1 || side == -1) c = bias[side == 1 ? a.dist.n - 1 : 0];
                     }
                     if (side == 0) {
 #pragma unroll
@@ -480,8 +469,11 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     if (!ROWS)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            reinterpret_cast<float *>(stat)[lane + 32 * i] = nl[i];
-                            reinterpret_cast<float *>(stat)[128 + lane + 32 * i] = nd[i];
+                            // (a row without keys: every exponential is 0; one number for the tile's bias goes into the LSE; columns
+                            // behind the last are masked, but must be finite)
+                            const bool in = lane + 32 * i < rows;
+                            reinterpret_cast<float *>(stat)[lane + 32 * i] = !in ? 0.f : L[i] == -INFINITY ? -INFINITY : c - L[i] * LOG2E;
+                            reinterpret_cast<float *>(stat)[128 + lane + 32 * i] = in ? -dl[i] * a.scale : 0.f;
                         }
                     if (side == 0)
 #pragma unroll
@@ -537,103 +529,69 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                 HDT_WAIT(bar, parity, site);
                 return HDT_AGREE();
             };
-            int nt0 = next_nt(), nt1 = nt0 > 0 ? next_nt() : 0, nt2 = nt1 > 0 ? next_nt() : 0, j = 0;
-            uint32_t uc = 0, st = 0, tp = 0;     // unit; ring stage of this tile and parity of its use
-            uint32_t sb = 0, sp = 0, par = 0;    // S buffer of the tile's first step and parity of its use; parity of the tile number
-            auto tile_wait = [&](uint32_t k, bool opens, uint32_t unit_no) {      // the tile k behind this one is there, and its unit's resident tiles
-                if (opens && !wait(RTM ? r_ready : r_full, unit_no & 1u, 4)) return false;
-                const bool wrap = st + k >= ST;
-                return wait(&t_full[wrap ? st + k - ST : st + k], wrap ? tp ^ 1u : tp, 5);
+            int nt = next_nt(), nt_n = nt > 0 ? next_nt() : 0, j = 0;
+            uint32_t uc = 0, st = 0, tp = 0, par = 0;      // unit; ring stage of this tile and parity of its use; parity of the tile number
+            auto put_s = [&](uint32_t x, uint32_t s_) {
+                issue_sdp(0, TM_S + 64u * x, x, s_);
+                mma_commit_p(leader, &s_full[x]);
             };
-            auto put_s = [&](uint32_t step, uint32_t x, uint32_t k) {      // S of the step `step` behind the tile's first, columns 64 x .. of the tile k behind
-                const uint32_t b = sb + step, b1 = b >= 2 * NSB ? b - 2 * NSB : b >= NSB ? b - NSB : b, s_ = st + k >= ST ? st + k - ST : st + k;
-                tc_fence_after();
-                issue_sdp(0, TM_S + 64u * b1, x, s_);
-                mma_commit_p(leader, &s_full[b1]);
-            };
-            auto put_dp = [&](uint32_t x, uint32_t k, bool last_of_unit) {
-                issue_sdp(1, TM_P + 64u * x, x, st + k >= ST ? st + k - ST : st + k);
+            auto put_dp = [&](uint32_t x, uint32_t s_, bool last_of_unit) {
+                issue_sdp(1, TM_P + 64u * x, x, s_);
                 mma_commit_p(leader, &dp_full[x]);
-                if (last_of_unit && x == 1) mma_commit_p(leader, RTM ? r_free : r_empty);      // the last that reads the resident tiles
+                if (x == 1 && last_of_unit) mma_commit_p(leader, RTM ? r_free : r_empty);      // the last that reads the resident tiles
             };
-            bool go = nt0 > 0 && tile_wait(0, true, 0);
+            bool go = nt > 0 && wait(RTM ? r_ready : r_full, 0, 4) && wait(&t_full[0], 0, 5);
             if (go) {
-                put_s(0, 0, 0);
-                put_s(1, 1, 0);
+                tc_fence_after();
+                put_s(0, 0);
+                put_s(1, 0);
                 put_dp(0, 0, false);
-                put_dp(1, 0, nt0 == 1);
-                if (NSB == 3 && (nt0 > 1 || nt1 > 0)) {
-                    go = tile_wait(1, nt0 == 1, 1);
-                    if (go) put_s(2, 0, 1);
-                }
+                put_dp(1, 0, nt == 1);
             }
-            while (go && nt0 > 0) {
-                const bool first = j == 0, last = j + 1 == nt0;
-                const bool more1 = !last || nt1 > 0, opens1 = last, last1 = last ? nt1 == 1 : j + 2 == nt0;      // the next tile
-                const bool more2 = more1 && (last1 ? (last ? nt2 : nt1) > 0 : true), opens2 = last1;              // the one behind it
-                // with one buffer of resident tiles in shared memory the next unit's come when this unit's last S and dP are through: its
-                // products go before the wait
-                const bool defer = !RTM && opens1;
-                if (first && uc > 0 && !wait(acc_free, (uc - 1) & 1u, 6)) break;
+            while (go && nt > 0) {
+                const bool last = j + 1 == nt, opens = last && nt_n > 0;      // the next tile opens a unit
+                const uint32_t s1 = st + 1 == ST ? 0 : st + 1, tp1 = st + 1 == ST ? tp ^ 1u : tp, acc = j == 0 ? 0u : 1u;
+                if (j == 0 && uc > 0 && !wait(acc_free, (uc - 1) & 1u, 6)) break;
 #pragma unroll
                 for (uint32_t x = 0; x < 2; ++x) {
-                    const bool wrap = sb + x >= NSB;
-                    const uint32_t b = wrap ? sb + x - NSB : sb + x;
-                    go = wait(&p_ready[b], wrap ? sp ^ 1u : sp, 7);
+                    go = wait(&p_ready[x], par, 7);
                     if (!go) break;
                     tc_fence_after();
-                    issue_acc(TM_ACC + D, TM_S + 64u * b, ROWS ? 0 : 1, x, st, first && x == 0 ? 0u : 1u);
-                    if (NSB == 3) {      // S three steps ahead, into the buffer that P has just been read from
+                    issue_acc(TM_ACC + D, TM_S + 64u * x, ROWS ? 0 : 1, x, st, x == 0 ? acc : 1u);
+                    if (!last) {
                         if (x == 0) {
-                            if (more1) put_s(3, 1, 1);
-                        } else if (more2 && !opens2) {
-                            go = tile_wait(2, false, 0);
-                            if (!go) break;
-                            put_s(4, 0, 2);
-                        }
-                    } else if (more1 && !defer) {
-                        if (x == 0) {
-                            go = tile_wait(1, false, 0);
+                            go = wait(&t_full[s1], tp1, 5);
                             if (!go) break;
                         }
-                        put_s(2 + x, x, 1);
+                        put_s(x, s1);
                     }
                     go = wait(&ds_ready[x], par, 8);
                     if (!go) break;
                     tc_fence_after();
-                    issue_acc(TM_ACC, TM_P + 64u * x, 0, x, st, first && x == 0 ? 0u : 1u);
-                    if (x == 1) {
-                        mma_commit_p(leader, &t_empty[st]);
-                        if (last) mma_commit_p(leader, acc_full);
-                    }
-                    if (more1 && !defer) put_dp(x, 1, last1);
+                    issue_acc(TM_ACC, TM_P + 64u * x, 0, x, st, x == 0 ? acc : 1u);
+                    if (x == 1) mma_commit_p(leader, &t_empty[st]);
+                    if (!last) put_dp(x, s1, j + 2 == nt);
                 }
                 if (!go) break;
-                if (NSB == 3) {
-                    if (more2 && opens2) {      // (its resident tiles follow the last dP of the unit before it)
-                        go = tile_wait(2, true, uc + (last ? 2u : 1u));
-                        if (go) put_s(4, 0, 2);
-                    }
-                } else if (more1 && defer) {
-                    go = tile_wait(1, true, uc + 1);
-                    if (go)
-#pragma unroll
-                        for (uint32_t x = 0; x < 2; ++x) {
-                            put_s(2 + x, x, 1);
-                            put_dp(x, 1, last1);
-                        }
-                }
-                if (++st == ST) { st = 0; tp ^= 1u; }
-                sb += 2;
-                if (sb >= NSB) { sb -= NSB; sp ^= 1u; }
-                par ^= 1u;
-                ++j;
                 if (last) {
-                    nt0 = nt1; nt1 = nt2;
-                    nt2 = nt1 > 0 ? next_nt() : 0;
+                    mma_commit_p(leader, acc_full);
+                    if (opens) {      // the next unit's resident tiles come behind this unit's last S and dP
+                        go = wait(RTM ? r_ready : r_full, (uc + 1) & 1u, 4) && wait(&t_full[s1], tp1, 5);
+                        if (!go) break;
+                        tc_fence_after();
+                        put_s(0, s1);
+                        put_s(1, s1);
+                        put_dp(0, s1, false);
+                        put_dp(1, s1, nt_n == 1);
+                    }
+                    nt = nt_n;
+                    nt_n = nt > 0 ? next_nt() : 0;
                     j = 0;
                     ++uc;
-                }
+                } else ++j;
+                st = s1;
+                tp = tp1;
+                par ^= 1u;
             }
         } else if (warp < W_LOAD) {
             // ================= drain group =================
