@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
     // resident tiles: loaded, free, in TMEM, read for the last time; walked tiles; S, dP; P, dS; accumulators; the rest
     uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 3, *s_full = bars + 4, *dp_full = bars + 6, *p_ready = bars + 8, *ds_ready = bars + 10;
     uint64_t *acc_full = bars + 12, *acc_free = bars + 13, *fix = bars + 14, *sum_full = bars + 15, *sum_free = bars + 16;
-    uint64_t *t_full = bars + 17, *t_empty = t_full + ST, *stat_full = t_empty + ST;
-    uint32_t *slot = (uint32_t *)(stat_full + ST);
+    uint64_t *t_full = bars + 17, *t_empty = t_full + ST;
+    uint32_t *slot = (uint32_t *)(t_empty + ST);
     volatile int *abort_flag = (volatile int *)(slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.H;
@@ -174,9 +174,8 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             mbar_init(&ds_ready[i], 256);
         }
         for (int i = 0; i < ST; ++i) {
-            mbar_init(&t_full[i], 1);
+            mbar_init(&t_full[i], 2);      // the tile's bytes; its statistics
             mbar_init(&t_empty[i], 1);
-            mbar_init(&stat_full[i], 1);
         }
         mbar_init(acc_full, 1);
         mbar_init(acc_free, 128);
@@ -239,6 +238,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 // (what a unit needs in its loop, and no more: p and d fill the registers)
                 int nt, base, first, end;      // tiles; distance of lane 0 and column 0; columns that this lane's row pairs with, from c0 on
+                int whole0, whole1;            // tiles in which every lane of the warp keeps all its columns
                 float row_l = 0.f, row_d = 0.f, by_side[2] = {0.f, 0.f};      // rows: -LSE' and -delta'; -LSE' with the bias of either side beyond the borders
                 {
                     const Unit U = unit(u);
@@ -261,6 +261,8 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     }
                     first -= U.c0 + c0;
                     end -= U.c0 + c0;
+                    whole0 = (max(__reduce_max_sync(0xffffffffu, first), 0) + 127) >> 7;
+                    whole1 = (__reduce_min_sync(0xffffffffu, end) - 32 + 128) >> 7;
                     if (ROWS && a.bias_on) {
                         by_side[0] = row_l + a.dist.bias[(size_t)U.h * a.dist.n];
                         by_side[1] = row_l + a.dist.bias[(size_t)(U.h + 1) * a.dist.n - 1];
@@ -272,16 +274,19 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     const int side = far_side(base);
                     base += ROWS ? -128 : 128;
                     const uint8_t *stat = sStat + st * Sh::STAT;
-                    const int jl = max(first, 0), jh = min(end, 32);
+                    uint32_t keep = 0xffffffffu;
+                    const bool all = j >= whole0 && j < whole1;
+                    bool any = true;
+                    if (!all) {
+                        const int jl = max(first, 0), jh = min(end, 32);
+                        keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
+                        any = __any_sync(0xffffffffu, keep != 0u);
+                    }
                     first -= 128;
                     end -= 128;
-                    const uint32_t keep = jh <= jl ? 0u : (jh >= 32 ? 0xffffffffu : (1u << jh) - 1u) & ~((1u << jl) - 1u);
-                    const bool any = __any_sync(0xffffffffu, keep != 0u), all = __all_sync(0xffffffffu, keep == 0xffffffffu);
                     const float l = !ROWS || side == 0 || side == 2 ? row_l : by_side[side == 1];
                     if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
-                    HDT_WAIT(&stat_full[st], tp, 11);
-                    HDT_WAIT(&s_full[x], par, 12);
-                    if (!HDT_AGREE()) break;
+                    HDT_WAIT(&s_full[x], par, 12);      // (a wait that ran out changes nothing in what the warp does before the tile's end)
                     tc_fence_after();
                     uint32_t p[32];
                     if (any) {
@@ -310,15 +315,17 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     tc_fence_before();
                     mbar_arrive(&p_ready[x]);
                     HDT_WAIT(&dp_full[x], par, 15);
-                    if (!HDT_AGREE()) break;
                     tc_fence_after();
                     float diag = 0.f;
+                    uint32_t d2[2][16];
+                    if (any && !ROWS) tmem_ld16(tm_dp, d2[0]);      // (rows: no room for a second load in flight)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        uint32_t d[16], y[8];
+                        uint32_t (&d)[16] = d2[i], y[8];
                         if (any) {
-                            tmem_ld16(tm_dp + 16u * i, d);
+                            if (ROWS) tmem_ld16(tm_dp + 16u * i, d);
                             tmem_wait_ld();
+                            if (!ROWS && i == 0) tmem_ld16(tm_dp + 16u, d2[1]);
                             const float *neg_d = reinterpret_cast<const float *>(stat) + 128 + c0 + 16 * i;
                             if (all) gradients<ROWS, false>(d, p + 16 * i, neg_d, row_d, a.scale, 0u);
                             else gradients<ROWS, true>(d, p + 16 * i, neg_d, row_d, a.scale, keep >> (16 * i));
@@ -368,6 +375,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     mbar_arrive(&ds_ready[x]);
                     if (++st == ST) { st = 0; tp ^= 1; }
                     par ^= 1;
+                    if (!HDT_AGREE()) break;
                     if (!(sums && side == 0 && any)) continue;
                     __syncwarp();
 #pragma unroll
@@ -482,7 +490,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                             stat[2048 + lane + 32 * i] = bk[i];
                         }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&stat_full[s]);
+                    if (lane == 0) mbar_arrive(&t_full[s]);
                     if (rows < 128) {
                         HDT_WAIT(fix, nfix & 1, 3);
                         ++nfix;
