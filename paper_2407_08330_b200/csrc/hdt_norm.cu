@@ -21,7 +21,7 @@
 namespace hdt {
 namespace {
 
-constexpr int THREADS = 128, BWD_CTAS = 4;
+constexpr int THREADS = 128;
 
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
@@ -51,6 +51,26 @@ __device__ __forceinline__ float row_sum(float v, float *s) {
         __syncthreads();
     }
     return v;
+}
+
+// Two sums at once; `turn` alternates from call to call, so that one barrier is enough.
+template <int LPR, int WPR>
+__device__ __forceinline__ void row_sums(float &a, float &b, float2 (&s)[2][WPR], int turn) {
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if constexpr (WPR > 1) {
+        if ((threadIdx.x & 31) == 0) s[turn][threadIdx.x >> 5] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.f;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) {
+            a += s[turn][w].x;
+            b += s[turn][w].y;
+        }
+    }
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
@@ -118,9 +138,9 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS) k_norm_fwd(const
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
-__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : BWD_CTAS) k_norm_bwd(const NormArgs a) {
+__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : WPR == 4 && NV == 1 ? 5 : 3) k_norm_bwd(const NormArgs a) {
     constexpr int NW = WPR > 4 ? WPR : THREADS / 32, RPC = WPR > 1 ? 1 : NW * (32 / LPR);   // rows of a CTA at a time
-    __shared__ float s_sum[WPR];
+    __shared__ float2 s_sum[2][WPR];
     __shared__ float s_col[WPR > 1 ? 1 : NW * 8 * 32];
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LPR;
@@ -133,17 +153,33 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : BW
         for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
     PhiloxKey key{0, 0, 0};
     if (a.drop.rng != nullptr) key = philox_key(a.drop);
-    for (int r0 = blockIdx.x * RPC; r0 < a.rows; r0 += gridDim.x * RPC) {
+    // the next row's dY and h are requested before this one's are looked at
+    Raw8<T, VEC> ng[NV], nx[NV];
+    auto request = [&](int r0) {
+        const size_t at = (size_t)min(r0 + sub, a.rows - 1) * a.cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            ng[i].template load<LPR>((const T *)a.dy + at, w0 + i * WPR, l, a.cols);
+            nx[i].template load<LPR>((const T *)a.hin + at, w0 + i * WPR, l, a.cols);
+        }
+    };
+    const int stride = gridDim.x * RPC;
+    int r0 = blockIdx.x * RPC, turn = 0;
+    if (r0 < a.rows) request(r0);
+    for (; r0 < a.rows; r0 += stride) {
         const bool on = r0 + sub < a.rows;
         const int row = on ? r0 + sub : a.rows - 1;
         const size_t at = (size_t)row * a.cols;
+        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
         float g[NV][8], x[NV][8];
+        Raw8<T, VEC> d[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            load8<LPR, VEC>((const T *)a.dy + at, w0 + i * WPR, l, a.cols, g[i]);
-            load8<LPR, VEC>((const T *)a.hin + at, w0 + i * WPR, l, a.cols, x[i]);
+            if (a.dh != nullptr) d[i].template load<LPR>((const T *)a.dh + at, w0 + i * WPR, l, a.cols);
+            ng[i].get(g[i]);
+            nx[i].get(x[i]);
         }
-        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
+        if (r0 + stride < a.rows) request(r0 + stride);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -162,13 +198,15 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : BW
                 s2 = fmaf(g[i][e], x[i][e], s2);
             }
         }
-        const float m1 = row_sum<LPR, WPR>(s1, s_sum) * inv, m2 = row_sum<LPR, WPR>(s2, s_sum) * inv;
+        row_sums<LPR, WPR>(s1, s2, s_sum, turn);
+        turn ^= 1;
+        const float m1 = s1 * inv, m2 = s2 * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float d[8];
-            if (a.dh != nullptr) load8<LPR, VEC>((const T *)a.dh + at, w0 + i * WPR, l, a.cols, d);
+            float y[8];
+            if (a.dh != nullptr) d[i].get(y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[i][e] = fmaf(g[i][e] - m1 - x[i][e] * m2, rstd, a.dh != nullptr ? d[e] : 0.f);
+            for (int e = 0; e < 8; ++e) g[i][e] = fmaf(g[i][e] - m1 - x[i][e] * m2, rstd, a.dh != nullptr ? y[e] : 0.f);
             if (on) store8<LPR, VEC>((T *)a.dres + at, w0 + i * WPR, l, a.cols, g[i]);
             if (a.drop.rng != nullptr) {
                 drop8<LPR, VEC>(key, a.drop, row, w0 + i * WPR, l, g[i]);
@@ -310,10 +348,35 @@ int norm_types(const NormArgs &a, int dtype, int w_dtype, bool vec, cudaStream_t
     return vec ? norm_pick<K, __nv_bfloat16, __nv_bfloat16, true>(a, st) : norm_pick<K, __nv_bfloat16, __nv_bfloat16, false>(a, st);
 }
 
-int rows_at_once(int cols) { return cols > 1024 ? 1 : cols > 128 ? 4 : cols > 64 ? 8 : cols > 32 ? 16 : 32; }
-// CTAs of the backward, and so partial rows: at most four to an SM.
+// The backward keeps two sums a column and the next row besides, so a warp holds a row of up to 768 (aligned bf16) or 512 columns,
+// four warps one of up to 2048, sixteen up to 8192 (1024 columns on one warp spilled 500 bytes a thread).
+template <template <typename, typename, bool, int, int, int> class K, typename T, typename W, bool VEC>
+int norm_pick_bwd(const NormArgs &a, cudaStream_t st) {
+    const int c = a.cols;
+    if (c <= 32) return K<T, W, VEC, 4, 1, 1>::go(a, st);
+    if (c <= 64) return K<T, W, VEC, 8, 1, 1>::go(a, st);
+    if (c <= 128) return K<T, W, VEC, 16, 1, 1>::go(a, st);
+    if (c <= 256) return K<T, W, VEC, 32, 1, 1>::go(a, st);
+    if (c <= 512) return K<T, W, VEC, 32, 1, 2>::go(a, st);
+    if constexpr (sizeof(T) == 2 && VEC)
+        if (c <= 768) return K<T, W, VEC, 32, 1, 3>::go(a, st);
+    if (c <= 1024) return K<T, W, VEC, 32, 4, 1>::go(a, st);
+    if (c <= 2048) return K<T, W, VEC, 32, 4, 2>::go(a, st);
+    if (c <= 4096) return K<T, W, VEC, 32, 16, 1>::go(a, st);
+    return K<T, W, VEC, 32, 16, 2>::go(a, st);
+}
+template <template <typename, typename, bool, int, int, int> class K>
+int norm_types_bwd(const NormArgs &a, int dtype, int w_dtype, bool vec, cudaStream_t st) {
+    if (dtype == HDT_F32) return vec ? norm_pick_bwd<K, float, float, true>(a, st) : norm_pick_bwd<K, float, float, false>(a, st);
+    if (w_dtype == HDT_F32) return vec ? norm_pick_bwd<K, __nv_bfloat16, float, true>(a, st) : norm_pick_bwd<K, __nv_bfloat16, float, false>(a, st);
+    return vec ? norm_pick_bwd<K, __nv_bfloat16, __nv_bfloat16, true>(a, st) : norm_pick_bwd<K, __nv_bfloat16, __nv_bfloat16, false>(a, st);
+}
+
+int rows_at_once(int cols) { return cols > 768 ? 1 : cols > 128 ? 4 : cols > 64 ? 8 : cols > 32 ? 16 : 32; }
+// CTAs of the backward, and so partial rows: those that are resident at once (any number is right).
 int bwd_grid(int64_t rows, int cols) {
-    const int64_t need = (rows + rows_at_once(cols) - 1) / rows_at_once(cols), most = cols > 4096 ? PLAN_SMS : BWD_CTAS * PLAN_SMS;
+    const int64_t need = (rows + rows_at_once(cols) - 1) / rows_at_once(cols);
+    const int64_t most = (int64_t)PLAN_SMS * (cols > 2048 ? 1 : cols > 1024 ? 3 : cols > 768 ? 5 : 3);
     return (int)(need < most ? need : most);
 }
 
@@ -412,7 +475,7 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
     cudaStream_t st = (cudaStream_t)stream;
     if (rows > 0) {
         const bool vec = cols % 8 == 0 && aligned16(d_y) && aligned16(d_h) && aligned16(h) && aligned16(weight) && aligned16(d_residual) && aligned16(d_x);
-        if (const int rc = norm_types<Bwd>(a, dtype, w_dtype, vec, st)) return rc;
+        if (const int rc = norm_types_bwd<Bwd>(a, dtype, w_dtype, vec, st)) return rc;
     }
     const int n = bwd_grid(rows, cols), ctas = (2 * cols + 31) / 32;
     if (w_dtype == HDT_F32) HDT_CUDA_CHECK(launch_dependent(k_norm_columns<float>, rows > 0, dim3(ctas), 1024, 0, st, a.part, n, cols, (float *)d_weight, (float *)d_bias));

@@ -11,6 +11,7 @@
 // A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
 #include <math.h>
 
+#include "hdt_rows.cuh"
 #include "hdt_self.cuh"
 
 namespace hdt {
@@ -198,24 +199,25 @@ __device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &
     return false;
 }
 template <bool BF16>
-struct Vec16 {      // 16 bytes of a row
-    static constexpr int E = BF16 ? 8 : 4;
-    uint4 x;
-    __device__ __forceinline__ void load(const void *p, size_t row16) { x = reinterpret_cast<const uint4 *>(p)[row16]; }
-    __device__ __forceinline__ float get(int e) const {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        if constexpr (BF16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-        else return __uint_as_float(w[e]);
+__device__ __forceinline__ void unpack16(const uint4 &x, f2 (&v)[BF16 ? 4 : 2]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    if constexpr (BF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = pack2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+    } else {
+        v[0] = pack2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        v[1] = pack2(__uint_as_float(w[2]), __uint_as_float(w[3]));
     }
-};
+}
 
+// (five CTAs to an SM: what step_piece deals out is resident at once)
 template <int D, bool BF16, int RG>
-__global__ void __launch_bounds__(128) k_self_step(const __grid_constant__ StepArgs a) {
-    using V = Vec16<BF16>;
-    constexpr int E = V::E, LPK = D / E, KPI = 32 / LPK, U = 4;
+__global__ void __launch_bounds__(128, RG == 1 ? 5 : 3) k_self_step(const __grid_constant__ StepArgs a) {
+    constexpr int E = BF16 ? 8 : 4, P = E / 2, LPK = D / E, KPI = 32 / LPK, U = 4;
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, l = lane % LPK, slot = lane / LPK;
     const int wid = blockIdx.x * 4 + (threadIdx.x >> 5), item = wid / a.H, h = wid % a.H;
+    const float far_bias = a.rel.on ? bias_base2(a.table, (size_t)self_bucket(a.rel, a.rel.far) * a.H + h, a.dtype) : 0.f;
     Doc d;
     int before;
     if (item >= a.items || !find_doc<RG, false>(a, item, d, before)) return;
@@ -225,27 +227,30 @@ __global__ void __launch_bounds__(128) k_self_step(const __grid_constant__ StepA
     const int kb = min(pc * cut.per, d.nk);
     int ke = min(kb + cut.per, d.nk);
     if (a.rel.causal) ke = max(kb, min(ke, pos0 + nr));
-    float q[RG][E], acc[RG][E], m[RG], s_l[RG];
+    f2 q[RG][P], acc[RG][P];
+    float m[RG], s_l[RG];
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
-        V x;
-        x.load(a.q, ((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * LPK + l);
+        unpack16<BF16>(reinterpret_cast<const uint4 *>(a.q)[((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * LPK + l], q[r]);
         m[r] = -INFINITY;
         s_l[r] = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            q[r][e] = x.get(e) * a.scale_log2;
-            acc[r][e] = 0.f;
+        for (int e = 0; e < P; ++e) {
+            q[r][e] = mul2(q[r][e], pack2(a.scale_log2, a.scale_log2));
+            acc[r][e] = pack2(0.f, 0.f);
         }
     }
-    const float far_bias = a.rel.on ? bias_base2(a.table, (size_t)self_bucket(a.rel, a.rel.far) * a.H + h, a.dtype) : 0.f;
+    const size_t step = (size_t)KPI * a.H * LPK;
+    const uint4 *kp = reinterpret_cast<const uint4 *>(a.k) + ((size_t)(d.k0 + kb + slot) * a.H + h) * LPK + l;
+    const uint4 *vp = reinterpret_cast<const uint4 *>(a.v) + ((size_t)(d.k0 + kb + slot) * a.H + h) * LPK + l;
     for (int k0 = kb; k0 < ke; k0 += KPI * U) {
-        V kx[U], vx[U];
+        uint4 kx[U], vx[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const size_t row = ((size_t)(d.k0 + min(k0 + u * KPI + slot, ke - 1)) * a.H + h) * LPK + l;
-            kx[u].load(a.k, row);
-            vx[u].load(a.v, row);
+        for (int u = 0; u < U; ++u) {      // (past the end: the piece's first key, weight 0)
+            const bool in = k0 + u * KPI + slot < ke;
+            const size_t o = in ? (size_t)(k0 - kb) / KPI * step + u * step : 0;
+            kx[u] = kp[in || kb + slot < ke ? o : 0 - (size_t)slot * a.H * LPK];
+            vx[u] = vp[in || kb + slot < ke ? o : 0 - (size_t)slot * a.H * LPK];
         }
 #pragma unroll
         for (int r = 0; r < RG; ++r) {
@@ -253,45 +258,59 @@ __global__ void __launch_bounds__(128) k_self_step(const __grid_constant__ StepA
             float s[U], top = m[r];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                s[u] = 0.f;
+                f2 x[P], t;
+                unpack16<BF16>(kx[u], x);
+                t = mul2(q[r][0], x[0]);
 #pragma unroll
-                for (int e = 0; e < E; ++e) s[u] = fmaf(q[r][e], kx[u].get(e), s[u]);
+                for (int e = 1; e < P; ++e) t = fma2(q[r][e], x[e], t);
+                float t0, t1;
+                unpack2(t, t0, t1);
+                s[u] = t0 + t1;
             }
 #pragma unroll
             for (int o = LPK / 2; o > 0; o >>= 1)
 #pragma unroll
                 for (int u = 0; u < U; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+            const bool plain = (!a.rel.on || pos0 + r - (k0 + U * KPI - 1) >= a.rel.far) && k0 + U * KPI <= ke && (!a.rel.causal || k0 + U * KPI - 1 <= pos0 + r);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int key = k0 + u * KPI + slot, dist = pos0 + r - key;
-                if (a.rel.on) s[u] += dist >= a.rel.far ? far_bias : bias_base2(a.table, (size_t)self_bucket(a.rel, dist) * a.H + h, a.dtype);
-                if (key >= ke || (a.rel.causal && dist < 0)) s[u] = -INFINITY;
+                if (plain) s[u] += far_bias;
+                else {
+                    const int key = k0 + u * KPI + slot, dist = pos0 + r - key;
+                    if (a.rel.on) s[u] += dist >= a.rel.far ? far_bias : bias_base2(a.table, (size_t)self_bucket(a.rel, dist) * a.H + h, a.dtype);
+                    if (key >= ke || (a.rel.causal && dist < 0)) s[u] = -INFINITY;
+                }
                 top = fmaxf(top, s[u]);
             }
             const float use = top == -INFINITY ? 0.f : top, f = exp2f(m[r] - use);
             m[r] = top;
             s_l[r] *= f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[r][e] *= f;
+            for (int e = 0; e < P; ++e) acc[r][e] = mul2(acc[r][e], pack2(f, f));
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const float p = exp2f(s[u] - use);
+                f2 x[P];
+                unpack16<BF16>(vx[u], x);
                 s_l[r] += p;
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(p, vx[u].get(e), acc[r][e]);
+                for (int e = 0; e < P; ++e) acc[r][e] = fma2(pack2(p, p), x[e], acc[r][e]);
             }
         }
     }
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
         if (r > 0 && r >= nr) break;
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < P; ++e) unpack2(acc[r][e], y[2 * e], y[2 * e + 1]);
 #pragma unroll
         for (int o = LPK; o < 32; o <<= 1) {      // the lane groups' softmaxes
             const float m2 = __shfl_xor_sync(0xffffffffu, m[r], o), top = fmaxf(m[r], m2), use = top == -INFINITY ? 0.f : top;
-            const float f = exp2f(m[r] - use), f2 = exp2f(m2 - use);
-            s_l[r] = s_l[r] * f + __shfl_xor_sync(0xffffffffu, s_l[r], o) * f2;
+            const float f = exp2f(m[r] - use), f2_ = exp2f(m2 - use);
+            s_l[r] = s_l[r] * f + __shfl_xor_sync(0xffffffffu, s_l[r], o) * f2_;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[r][e] = acc[r][e] * f + __shfl_xor_sync(0xffffffffu, acc[r][e], o) * f2;
+            for (int e = 0; e < E; ++e) y[e] = y[e] * f + __shfl_xor_sync(0xffffffffu, y[e], o) * f2_;
             m[r] = top;
         }
         if (lane >= LPK) continue;
@@ -303,61 +322,90 @@ __global__ void __launch_bounds__(128) k_self_step(const __grid_constant__ StepA
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(acc[r][2 * e] * inv, acc[r][2 * e + 1] * inv);
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(y[2 * e] * inv, y[2 * e + 1] * inv);
                     w[e] = *reinterpret_cast<const uint32_t *>(&p);
                 }
                 *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.o + at) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else *reinterpret_cast<float4 *>((float *)a.o + at) = make_float4(acc[r][0] * inv, acc[r][1] * inv, acc[r][2] * inv, acc[r][3] * inv);
+            } else *reinterpret_cast<float4 *>((float *)a.o + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
             if (l == 0) a.lse[(size_t)h * a.Tq + row] = s_l[r] == 0.f ? -INFINITY : (m[r] + log2f(s_l[r])) * 0.6931471805599453f;
         } else {
             const size_t at = ((size_t)item * RG + r) * a.H + h;
 #pragma unroll
-            for (int e = 0; e < E; e += 4)
-                *reinterpret_cast<float4 *>(a.part_o + at * D + l * E + e) = make_float4(acc[r][e], acc[r][e + 1], acc[r][e + 2], acc[r][e + 3]);
+            for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(a.part_o + at * D + l * E + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
             if (l == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(m[r], s_l[r]);
         }
     }
 }
 
-// The pieces of a row, a warp per (row, head).
+// The pieces of a row, a CTA per (row, head): its four warps take every fourth piece, four of them in flight, and meet in order.
 template <int D, bool BF16, int RG>
 __global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepArgs a) {
     constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31, wid = blockIdx.x * 4 + (threadIdx.x >> 5), row = wid / a.H, h = wid % a.H;
+    __shared__ float s_acc[4][D], s_ml[4][2];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x / a.H, h = blockIdx.x % a.H;
     Doc d;
     int before;
     // (before the wait: the kernel in front does not write the offsets, and began behind what did)
-    const bool found = row < a.Tq && find_doc<RG, true>(a, row, d, before);
+    const bool found = find_doc<RG, true>(a, row, d, before);
     pdl_wait();
     if (!found) return;
     const StepDoc<RG> cut(d, a.piece);
     const int r = row - d.q0, first = before + (r / RG) * cut.pieces;
     if (cut.pieces == 1 || first + cut.pieces > a.items) return;      // written by the one warp that had the row (or no valid offsets)
     auto at = [&](int i) { return ((size_t)(first + i) * RG + r % RG) * a.H + h; };
-    float top = -INFINITY;
-    for (int i = lane; i < cut.pieces; i += 32) top = fmaxf(top, a.part_ml[at(i) * 2]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float use = top == -INFINITY ? 0.f : top;
-    float l = 0.f, acc[E];
+    float m = -INFINITY, l = 0.f, acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < cut.pieces; ++i) {
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2);
-        const float f = exp2f(ml.x - use);
-        l += ml.y * f;
+    for (int i0 = w; i0 < cut.pieces; i0 += 16) {
+        float2 ml[4];
+        float x[4][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(a.part_o[at(i) * D + lane * E + e], f, acc[e]);
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const size_t out = ((size_t)row * a.H + h) * D + lane * E;
+        for (int u = 0; u < 4; ++u) {
+            const int i = min(i0 + 4 * u, cut.pieces - 1);
+            ml[u] = *reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        if constexpr (BF16) ((__nv_bfloat16 *)a.o)[out + e] = __float2bfloat16(acc[e] * inv);
-        else ((float *)a.o)[out + e] = acc[e] * inv;
+            for (int e = 0; e < E; ++e) x[u][e] = a.part_o[at(i) * D + lane * E + e];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + 4 * u >= cut.pieces) ml[u] = make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, ml[u].x);
+        }
+        const float use = top == -INFINITY ? 0.f : top, f = exp2f(m - use);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float f = exp2f(ml[u].x - use);
+            l += ml[u].y * f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], f, acc[e]);
+        }
     }
-    if (lane == 0) a.lse[(size_t)h * a.Tq + row] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_acc[w][lane * E + e] = acc[e];
+    if (lane == 0) { s_ml[w][0] = m; s_ml[w][1] = l; }
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float top = -INFINITY, y = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, s_ml[i][0]);
+    const float use = top == -INFINITY ? 0.f : top;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float f = exp2f(s_ml[i][0] - use);
+        l += s_ml[i][1] * f;
+        y = fmaf(s_acc[i][threadIdx.x], f, y);
+    }
+    y *= l == 0.f ? 0.f : 1.f / l;
+    const size_t out = ((size_t)row * a.H + h) * D + threadIdx.x;
+    if constexpr (BF16) ((__nv_bfloat16 *)a.o)[out] = __float2bfloat16(y);
+    else ((float *)a.o)[out] = y;
+    if (threadIdx.x == 0) a.lse[(size_t)h * a.Tq + row] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -480,7 +528,7 @@ int step_go(StepArgs a, cudaStream_t st) {
     a.items = (int)step_items(a.B, a.Tq, a.Tk, a.H, RG);
     HDT_CUDA_CHECK(launch_dependent(k_self_step<D, BF16, RG>, false, dim3((unsigned)(((long long)a.items * a.H + 3) / 4)), 128, 0, st, a));
     if (a.Tk <= a.piece) return HDT_OK;      // no document of several pieces
-    HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)(((long long)a.Tq * a.H + 3) / 4)), 128, 0, st, a));
+    HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)a.Tq * (unsigned)a.H), 128, 0, st, a));
     return HDT_OK;
 }
 template <int D, bool BF16>

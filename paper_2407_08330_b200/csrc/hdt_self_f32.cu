@@ -17,16 +17,20 @@ constexpr int R = SELF_F32_ROWS, PS = R + 4;      // row stride of a transposed 
 template <int D>
 struct Shape { static constexpr int XS = D + 4, X = R * XS; };
 
-// 64 rows of [T, H, D] from `row` on, those behind `n` as zeros.
+// 64 rows of [T, H, D] from `row` on, those behind `n` as zeros: requested here, there after `arrived`.
 template <int D>
-__device__ __forceinline__ void load_rows(float *dst, const float *src, int row, int n, int h, int H) {
+__device__ __forceinline__ void request_rows(float *dst, const float *src, int row, int n, int h, int H) {
+#pragma unroll
     for (int i = threadIdx.x; i < R * (D / 4); i += 256) {
         const int r = i / (D / 4), c = 4 * (i % (D / 4));
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < n) x = *reinterpret_cast<const float4 *>(src + ((size_t)(row + r) * H + h) * D + c);
-        *reinterpret_cast<float4 *>(dst + r * Shape<D>::XS + c) = x;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + r * Shape<D>::XS + c);
+        const float *from = src + ((size_t)(row + min(r, n - 1)) * H + h) * D + c;      // (n > 0)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(r < n ? 16 : 0) : "memory");
     }
 }
+__device__ __forceinline__ void requested() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 // s[i][j] = a row (ty + 16 i) . b row (tx + 16 j)
 template <int D>
 __device__ __forceinline__ void dots(const float *a, const float *b, int ty, int tx, float (&s)[4][4]) {
@@ -87,15 +91,24 @@ __device__ __forceinline__ void store_rows(float *dst, const float (&acc)[4][D /
 template <int D>
 __global__ void __launch_bounds__(256) k_self_fwd_f32(const SelfFwdArgs a) {
     extern __shared__ float sm[];
-    float *sQ = sm, *sK = sQ + Shape<D>::X, *sV = sK + Shape<D>::X, *sP = sV + Shape<D>::X, *sF = sP + R * PS, *sNb = sF + R;
+    constexpr int X = Shape<D>::X;
+    float *sQ = sm, *sKV = sQ + X, *sP = sKV + 4 * X, *sF = sP + R * PS, *sNb = sF + R;      // K and V twice
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15, H = a.H;
     pdl_wait();
     const int n_units = *a.q.count * H;
     for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
         const SelfBlk b = a.q.blk[u / H];
         const int h = u % H, rows = min(R, b.nq - b.r0), keys = self_keys_of(a.causal, b.r0, R, b.nq, b.nk);
+        auto request = [&](int k, int to) {
+            request_rows<D>(sKV + 2 * to * X, (const float *)a.kp, b.k0 + k, b.nk - k, h, H);
+            request_rows<D>(sKV + (2 * to + 1) * X, (const float *)a.vp, b.k0 + k, b.nk - k, h, H);
+            requested();
+        };
         __syncthreads();
-        load_rows<D>(sQ, (const float *)a.qp, b.q0 + b.r0, rows, h, H);
+        if (keys > 0) {
+            request_rows<D>(sQ, (const float *)a.qp, b.q0 + b.r0, rows, h, H);
+            request(0, 0);
+        }
         float acc[4][D / 16], m[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -104,11 +117,14 @@ __global__ void __launch_bounds__(256) k_self_fwd_f32(const SelfFwdArgs a) {
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) acc[i][c] = 0.f;
         }
-        for (int k = 0; k < keys; k += R) {
-            __syncthreads();
-            load_rows<D>(sK, (const float *)a.kp, b.k0 + k, b.nk - k, h, H);
-            load_rows<D>(sV, (const float *)a.vp, b.k0 + k, b.nk - k, h, H);
+        for (int k = 0, at = 0; k < keys; k += R, at ^= 1) {
+            const float *sK = sKV + 2 * at * X, *sV = sK + X;
+            __syncthreads();                    // (the other buffer, P and the bias have been read)
             if (a.bias_on) load_near(sNb, a.dist, h, b.off + b.r0 - k);
+            if (k + R < keys) {
+                request(k + R, at ^ 1);
+                arrived<1>();
+            } else arrived<0>();
             __syncthreads();
             float s[4][4];
             dots<D>(sQ, sK, ty, tx, s);
@@ -171,8 +187,10 @@ __global__ void __launch_bounds__(256) k_self_fwd_f32(const SelfFwdArgs a) {
 template <int D, bool ROWS>
 __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
     extern __shared__ float sm[];
-    float *sA = sm, *sB = sA + Shape<D>::X, *sX = sB + Shape<D>::X, *sY = sX + Shape<D>::X, *sP = sY + Shape<D>::X, *sD = sP + (ROWS ? 0 : R * PS);
+    constexpr int X = Shape<D>::X, NBUF = D == 64 ? 2 : 1;      // (two buffers of walked tiles do not fit at head_dim 128)
+    float *sA = sm, *sB = sA + X, *sXY = sB + X, *sP = sXY + 2 * NBUF * X, *sD = sP + (ROWS ? 0 : R * PS);
     float *sL = sD + R * PS, *sDel = sL + R, *sNb = sDel + R, *sDiag = sNb + 2 * R;
+    int *sBk = (int *)(sDiag + 2 * R);
     const int t = threadIdx.x, ty = t >> 4, tx = t & 15, H = a.H;
     const float LOG2E = 1.4426950408889634f;
     pdl_wait();
@@ -183,9 +201,17 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
         const int h = u % H, rows = min(R, (ROWS ? b.nq : b.nk) - b.r0);
         const int c0 = ROWS ? 0 : self_first_row(a.causal, b.r0, b.nq, b.nk), c1 = ROWS ? self_keys_of(a.causal, b.r0, R, b.nq, b.nk) : b.nq;
         const int a0 = (ROWS ? b.q0 : b.k0) + b.r0, x0 = ROWS ? b.k0 : b.q0;
+        auto request = [&](int c, int to) {
+            request_rows<D>(sXY + 2 * to * X, (const float *)(ROWS ? a.kp : a.qp), x0 + c, c1 - c, h, H);
+            request_rows<D>(sXY + (2 * to + 1) * X, (const float *)(ROWS ? a.vp : a.dop), x0 + c, c1 - c, h, H);
+            requested();
+        };
         __syncthreads();
-        load_rows<D>(sA, (const float *)(ROWS ? a.qp : a.kp), a0, rows, h, H);
-        load_rows<D>(sB, (const float *)(ROWS ? a.dop : a.vp), a0, rows, h, H);
+        if (c0 < c1) {
+            request_rows<D>(sA, (const float *)(ROWS ? a.qp : a.kp), a0, rows, h, H);
+            request_rows<D>(sB, (const float *)(ROWS ? a.dop : a.vp), a0, rows, h, H);
+            request(c0, 0);
+        }
         auto stats = [&](int row, int n) {      // LSE' and delta of 64 query rows
             if (t >= R) return;
             const size_t r = (size_t)h * a.Tq + row + t;
@@ -194,7 +220,7 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
             sDel[t] = t < n ? a.delta[r] : 0.f;
         };
         if (ROWS) stats(a0, rows);
-        float acc1[4][D / 16], acc2[4][ROWS ? 1 : D / 16], by_bucket = 0.f;
+        float acc1[4][D / 16], acc2[4][ROWS ? 1 : D / 16], by_bucket = 0.f, far_sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -202,13 +228,21 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
 #pragma unroll
             for (int c = 0; c < (ROWS ? 1 : D / 16); ++c) acc2[i][c] = 0.f;
         }
-        for (int c = c0; c < c1; c += R) {
-            __syncthreads();
-            load_rows<D>(sX, (const float *)(ROWS ? a.kp : a.qp), x0 + c, c1 - c, h, H);
-            load_rows<D>(sY, (const float *)(ROWS ? a.vp : a.dop), x0 + c, c1 - c, h, H);
-            if (!ROWS) stats(x0 + c, c1 - c);
+        for (int c = c0, at = 0; c < c1; c += R, at ^= NBUF - 1) {
+            const float *sX = sXY + 2 * at * X, *sY = sX + X;
             const int base = ROWS ? b.off + b.r0 - c : b.off + c - b.r0;      // distance of row 0 and column 0
+            const int side = !a.bias_on ? 2 : base - (R - 1) >= a.dist.far ? 1 : base + (R - 1) <= -a.dist.far ? -1 : 0;
+            __syncthreads();
+            if (!ROWS) stats(x0 + c, c1 - c);
             if (a.bias_on) load_near(sNb, a.dist, h, base);
+            if (ROWS && a.part != nullptr && side == 0 && t < 2 * R) sBk[t] = a.dist.bucket[self_dist_at(a.dist, base + t - (R - 1))];
+            if (NBUF == 2 && c + R < c1) {
+                request(c + R, at ^ 1);
+                arrived<1>();
+            } else {
+                if (NBUF == 1 && c > c0) request(c, 0);
+                arrived<0>();
+            }
             __syncthreads();
             float s[4][4], d[4][4];
             dots<D>(sA, sX, ty, tx, s);
@@ -222,12 +256,13 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
                     const float y = fmaf(s[i][j], a.scale_log2, a.bias_on ? sNb[R - 1 + step] : 0.f) - sL[q];
                     const float p = keep ? exp2f(y) : 0.f, ds = keep ? p * (d[i][j] - sDel[q]) : 0.f;
                     if (!ROWS) sP[k * PS + r] = p;
+                    else if (side == 1 || side == -1) far_sum[side == -1] += ds;
                     sD[k * PS + r] = ds;
                 }
             __syncthreads();
             accumulate<D>(sD, sX, ty, tx, acc1);
             if constexpr (!ROWS) accumulate<D>(sP, sY, ty, tx, acc2);
-            if (ROWS && a.part != nullptr) {
+            if (ROWS && a.part != nullptr && side == 0) {
                 if (t < 2 * R - 1) {      // the diagonal row - column = t - 63
                     float v = 0.f;
                     for (int r = max(0, t - (R - 1)); r < min(R, t + 1); ++r) v += sD[(r - (t - (R - 1))) * PS + r];
@@ -235,9 +270,22 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
                 }
                 __syncthreads();
                 if (t < a.buckets)
-                    for (int i = 0; i < 2 * R - 1; ++i)
-                        if (a.dist.bucket[self_dist_at(a.dist, base + i - (R - 1))] == t) by_bucket += sDiag[i];
+#pragma unroll 4
+                    for (int i = 0; i < 2 * R - 1; ++i) by_bucket += sBk[i] == t ? sDiag[i] : 0.f;
             }
+        }
+        if (ROWS && a.part != nullptr) {      // the sums beyond the last borders: over the warps in order
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) far_sum[g] += __shfl_xor_sync(0xffffffffu, far_sum[g], o);
+                if ((t & 31) == 0) sDiag[8 * g + (t >> 5)] = far_sum[g];
+            }
+            __syncthreads();
+            for (int g = 0; g < 2; ++g)
+                if (t == a.dist.bucket[g == 0 ? a.dist.n - 1 : 0])
+                    for (int i = 0; i < 8; ++i) by_bucket += sDiag[8 * g + i];
         }
         const float scale = a.scale;
 #pragma unroll
@@ -256,7 +304,7 @@ __global__ void __launch_bounds__(256) k_self_bwd_f32(const SelfBwdArgs a) {
 
 template <int D>
 int fwd(const SelfFwdArgs &a, cudaStream_t st) {
-    constexpr int smem = (3 * Shape<D>::X + R * PS + R + 2 * R) * 4;
+    constexpr int smem = (5 * Shape<D>::X + R * PS + R + 2 * R) * 4;
     static DevOnce attr;
     if (!attr.done()) {
         HDT_CUDA_CHECK(cudaFuncSetAttribute(k_self_fwd_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
@@ -270,7 +318,7 @@ int fwd(const SelfFwdArgs &a, cudaStream_t st) {
 }
 template <int D, bool ROWS>
 int bwd(const SelfBwdArgs &a, cudaStream_t st) {
-    constexpr int smem = (4 * Shape<D>::X + (ROWS ? 1 : 2) * R * PS + 2 * R + 2 * R + 2 * R) * 4;
+    constexpr int smem = ((D == 64 ? 6 : 4) * Shape<D>::X + (ROWS ? 1 : 2) * R * PS + 2 * R + 2 * R + 2 * R + 2 * R) * 4;
     static DevOnce attr;
     if (!attr.done()) {
         HDT_CUDA_CHECK(cudaFuncSetAttribute(k_self_bwd_f32<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));

@@ -220,7 +220,7 @@ def test_many_short_documents(dtype, d, causal):
     """Several units of one tile, and of none, in a row for every CTA."""
     lens = [(37 * i) % 150 for i in range(90)]
     keys = [0 if i % 11 == 0 else n + (i % 3) * 40 for i, n in enumerate(lens)]
-    c = Case(lens, keys, 12, d, dtype, causal)
+    c = Case(lens, keys, 5, d, dtype, causal)
     c.check(c.run())
 
 
