@@ -6,9 +6,8 @@
 // vector of it and nobody looks for buckets again.  Latency: 4 x 4096 tokens about 5 us.
 //
 // Decoding (few rows per document): bound by HBM, the keys and values once.  A warp takes a piece of a document's keys for
-// one head and up to four rows; a key is read by D / 8 (bf16) or D / 4 (fp32) lanes, 16 bytes each, four keys per lane
-// group in flight; every lane group has a softmax of its own, joined at the piece's end, the pieces by k_self_join.
-// A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
+// one head and up to four rows; every lane group has a softmax of its own, joined at the piece's end, the pieces by
+// k_self_join.  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
 #include <math.h>
 
 #include "hdt_rows.cuh"
@@ -198,24 +197,16 @@ __device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &
     }
     return false;
 }
-template <bool BF16>
-__device__ __forceinline__ void unpack16(const uint4 &x, f2 (&v)[BF16 ? 4 : 2]) {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    if constexpr (BF16) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = pack2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-    } else {
-        v[0] = pack2(__uint_as_float(w[0]), __uint_as_float(w[1]));
-        v[1] = pack2(__uint_as_float(w[2]), __uint_as_float(w[3]));
-    }
-}
-
-// (five CTAs to an SM: what step_piece deals out is resident at once)
+// A key's row lies on D / 8 lanes, a lane group has four keys at a time (and, one row, bf16, the next four in flight); each lane keeps the
+// score of one of them, so an exponential is computed twice or four times and not by every lane.
 template <int D, bool BF16, int RG>
-__global__ void __launch_bounds__(128, RG == 1 ? 5 : 3) k_self_step(const __grid_constant__ StepArgs a) {
-    constexpr int E = BF16 ? 8 : 4, P = E / 2, LPK = D / E, KPI = 32 / LPK, U = 4;
+__global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid_constant__ StepArgs a) {
+    constexpr int LPK = D / 8, KPI = 32 / LPK, C = 4;
+    using W = Raw<BF16, LPK>;
+    constexpr size_t ROW = D * (BF16 ? 2 : 4);
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, l = lane % LPK, slot = lane / LPK;
+    const int lane = threadIdx.x & 31, l = lane % LPK, slot = lane / LPK, src = lane - l;
+    const unsigned mask = 0xffffffffu;
     const int wid = blockIdx.x * 4 + (threadIdx.x >> 5), item = wid / a.H, h = wid % a.H;
     const float far_bias = a.rel.on ? bias_base2(a.table, (size_t)self_bucket(a.rel, a.rel.far) * a.H + h, a.dtype) : 0.f;
     Doc d;
@@ -227,112 +218,73 @@ __global__ void __launch_bounds__(128, RG == 1 ? 5 : 3) k_self_step(const __grid
     const int kb = min(pc * cut.per, d.nk);
     int ke = min(kb + cut.per, d.nk);
     if (a.rel.causal) ke = max(kb, min(ke, pos0 + nr));
-    f2 q[RG][P], acc[RG][P];
-    float m[RG], s_l[RG];
+    constexpr bool AHEAD = RG == 1 && BF16;      // (else the registers do not hold the next four keys)
+    W q[RG], x[C], y[C], x1[AHEAD ? C : 1], y1[AHEAD ? C : 1];
+    RowSoftmax S[RG];
+    const char *kp = (const char *)a.k + ((size_t)d.k0 * a.H + h) * ROW, *vp = (const char *)a.v + ((size_t)d.k0 * a.H + h) * ROW;
+    auto request = [&](int k0, W (&kx)[C], W (&vx)[C]) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {      // (past the end: the last key, weight 0)
+            const size_t o = (size_t)min(k0 + slot * C + c, ke - 1) * a.H * ROW;
+            kx[c].load(kp + o, 0u, l);
+            vx[c].load(vp + o, 0u, l);
+        }
+    };
+    if constexpr (AHEAD)
+        if (kb < ke) request(kb, x1, y1);
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
-        unpack16<BF16>(reinterpret_cast<const uint4 *>(a.q)[((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * LPK + l], q[r]);
-        m[r] = -INFINITY;
-        s_l[r] = 0.f;
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-            q[r][e] = mul2(q[r][e], pack2(a.scale_log2, a.scale_log2));
-            acc[r][e] = pack2(0.f, 0.f);
-        }
+        q[r].load((const char *)a.q + ((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * ROW, 0u, l);
+        S[r].clear();
     }
-    const size_t step = (size_t)KPI * a.H * LPK;
-    const uint4 *kp = reinterpret_cast<const uint4 *>(a.k) + ((size_t)(d.k0 + kb + slot) * a.H + h) * LPK + l;
-    const uint4 *vp = reinterpret_cast<const uint4 *>(a.v) + ((size_t)(d.k0 + kb + slot) * a.H + h) * LPK + l;
-    for (int k0 = kb; k0 < ke; k0 += KPI * U) {
-        uint4 kx[U], vx[U];
+    for (int k0 = kb; k0 < ke; k0 += KPI * C) {
+        if constexpr (AHEAD) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {      // (past the end: the piece's first key, weight 0)
-            const bool in = k0 + u * KPI + slot < ke;
-            const size_t o = in ? (size_t)(k0 - kb) / KPI * step + u * step : 0;
-            kx[u] = kp[in || kb + slot < ke ? o : 0 - (size_t)slot * a.H * LPK];
-            vx[u] = vp[in || kb + slot < ke ? o : 0 - (size_t)slot * a.H * LPK];
-        }
+            for (int c = 0; c < C; ++c) {
+                x[c] = x1[c];
+                y[c] = y1[c];
+            }
+            if (k0 + KPI * C < ke) request(k0 + KPI * C, x1, y1);
+        } else request(k0, x, y);
+        const int key = k0 + slot * C + (l & (C - 1));                  // the key whose score this lane keeps
 #pragma unroll
         for (int r = 0; r < RG; ++r) {
-            if (r > 0 && r >= nr) break;
-            float s[U], top = m[r];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                f2 x[P], t;
-                unpack16<BF16>(kx[u], x);
-                t = mul2(q[r][0], x[0]);
-#pragma unroll
-                for (int e = 1; e < P; ++e) t = fma2(q[r][e], x[e], t);
-                float t0, t1;
-                unpack2(t, t0, t1);
-                s[u] = t0 + t1;
-            }
-#pragma unroll
-            for (int o = LPK / 2; o > 0; o >>= 1)
-#pragma unroll
-                for (int u = 0; u < U; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
-            const bool plain = (!a.rel.on || pos0 + r - (k0 + U * KPI - 1) >= a.rel.far) && k0 + U * KPI <= ke && (!a.rel.causal || k0 + U * KPI - 1 <= pos0 + r);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (plain) s[u] += far_bias;
-                else {
-                    const int key = k0 + u * KPI + slot, dist = pos0 + r - key;
-                    if (a.rel.on) s[u] += dist >= a.rel.far ? far_bias : bias_base2(a.table, (size_t)self_bucket(a.rel, dist) * a.H + h, a.dtype);
-                    if (key >= ke || (a.rel.causal && dist < 0)) s[u] = -INFINITY;
-                }
-                top = fmaxf(top, s[u]);
-            }
-            const float use = top == -INFINITY ? 0.f : top, f = exp2f(m[r] - use);
-            m[r] = top;
-            s_l[r] *= f;
-#pragma unroll
-            for (int e = 0; e < P; ++e) acc[r][e] = mul2(acc[r][e], pack2(f, f));
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float p = exp2f(s[u] - use);
-                f2 x[P];
-                unpack16<BF16>(vx[u], x);
-                s_l[r] += p;
-#pragma unroll
-                for (int e = 0; e < P; ++e) acc[r][e] = fma2(pack2(p, p), x[e], acc[r][e]);
-            }
+            float sc[C];
+            dots<C>(q[r], x, sc);
+            float s = reduce_scatter<C, LPK>(sc, l, mask) * a.scale_log2;
+            const int dist = pos0 + r - key;
+            if (a.rel.on) s += dist >= a.rel.far ? far_bias : bias_base2(a.table, (size_t)self_bucket(a.rel, dist) * a.H + h, a.dtype);
+            if (key >= ke || (a.rel.causal && dist < 0)) s = -INFINITY;
+            const float p = S[r].template add<C>(s, mask);
+            axpys<C>(S[r].acc, p, y, mask, src);
         }
     }
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
         if (r > 0 && r >= nr) break;
-        float y[E];
 #pragma unroll
-        for (int e = 0; e < P; ++e) unpack2(acc[r][e], y[2 * e], y[2 * e + 1]);
+        for (int o = 1; o < C; o *= 2) S[r].l += __shfl_xor_sync(mask, S[r].l, o);
 #pragma unroll
         for (int o = LPK; o < 32; o <<= 1) {      // the lane groups' softmaxes
-            const float m2 = __shfl_xor_sync(0xffffffffu, m[r], o), top = fmaxf(m[r], m2), use = top == -INFINITY ? 0.f : top;
-            const float f = exp2f(m[r] - use), f2_ = exp2f(m2 - use);
-            s_l[r] = s_l[r] * f + __shfl_xor_sync(0xffffffffu, s_l[r], o) * f2_;
+            f2 z[4];
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = y[e] * f + __shfl_xor_sync(0xffffffffu, y[e], o) * f2_;
-            m[r] = top;
+            for (int u = 0; u < 4; ++u) z[u] = __shfl_xor_sync(mask, S[r].acc[u], o);
+            const float m2 = __shfl_xor_sync(mask, S[r].m, o), l2 = __shfl_xor_sync(mask, S[r].l, o);
+            S[r].merge(m2, l2, z);
         }
         if (lane >= LPK) continue;
         const int row = d.q0 + r0 + r;
         if (cut.pieces == 1) {
-            const float inv = s_l[r] == 0.f ? 0.f : 1.f / s_l[r];
-            const size_t at = ((size_t)row * a.H + h) * D + l * E;
-            if constexpr (BF16) {
-                uint32_t w[4];
+            // (a sum that is no number stays one)
+            const float inv = S[r].l == 0.f ? 0.f : 1.f / S[r].l;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(y[2 * e] * inv, y[2 * e + 1] * inv);
-                    w[e] = *reinterpret_cast<const uint32_t *>(&p);
-                }
-                *reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.o + at) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else *reinterpret_cast<float4 *>((float *)a.o + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-            if (l == 0) a.lse[(size_t)h * a.Tq + row] = s_l[r] == 0.f ? -INFINITY : (m[r] + log2f(s_l[r])) * 0.6931471805599453f;
+            for (int u = 0; u < 4; ++u) S[r].acc[u] = mul2(S[r].acc[u], pack2(inv, inv));
+            W::store((char *)a.o + ((size_t)row * a.H + h) * ROW, 0u, l, S[r].acc);
+            if (l == 0) a.lse[(size_t)h * a.Tq + row] = S[r].l == 0.f ? -INFINITY : (S[r].m + log2f(S[r].l)) * 0.6931471805599453f;
         } else {
             const size_t at = ((size_t)item * RG + r) * a.H + h;
-#pragma unroll
-            for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(a.part_o + at * D + l * E + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-            if (l == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(m[r], s_l[r]);
+            Raw<BF16, LPK>::store_f32(a.part_o + at * D, 0, l, S[r].acc);
+            if (l == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(S[r].m, S[r].l);
         }
     }
 }
@@ -450,9 +402,9 @@ void rel_fill(SelfRel *r, int buckets, int max_distance, int causal) {
 size_t al(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which a call is a step of decoding
 bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
-// Keys of a piece: sixteen warps to an SM if the rows are one per document, at least 64.
+// Keys of a piece: fourteen warps to an SM if the rows are one per document (sixteen fit at once, and documents round up), at least 64.
 int step_piece(int Tk, int H) {
-    const long long per = ((long long)Tk * H + 16 * PLAN_SMS - 1) / (16 * PLAN_SMS);
+    const long long per = ((long long)Tk * H + 14 * PLAN_SMS - 1) / (14 * PLAN_SMS);
     return (int)((per < 64 ? 64 : per) + 15) / 16 * 16;
 }
 // (a document of g row groups has at most keys / piece + g items)
