@@ -16,6 +16,7 @@
 //
 // The rows of V behind a document's last key are set to zero in shared memory: P is 0 there, but another document's rows,
 // or a cache's unused ones, may hold NaN.
+#include "hdt_rows.cuh"
 #include "hdt_self.cuh"
 #include "hdt_sm100.cuh"
 #include "hdt_tmap.cuh"
@@ -111,6 +112,7 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                 const int first = b.off + b.r0 + 128 * w;      // position of the tile's first row
                 const int lim0 = !valid ? 0 : a.causal ? min(max(b.off + row + 1, 0), b.nk) : b.nk;
                 const float *bias = a.dist.bias + (size_t)h * a.dist.n;
+                const int whole = __reduce_min_sync(0xffffffffu, lim0) >> 7;      // tiles that every row of the warp sees whole
                 float m = -INFINITY, l = 0.f;
                 for (int j = 0; j < nt; ++j, ++ns) {
                     const int base = first - 128 * j, lim = lim0 - 128 * j;
@@ -140,10 +142,13 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                     if (near) {
                         const float *nr = nb + rl + 127;
 #pragma unroll
-                        for (int i = 0; i < 128; ++i) s[i] = fmaf(s[i], sl, nr[-i]);
+                        for (int i = 0; i < 128; i += 2) {
+                            const f2 x = fma2(pack2(s[i], s[i + 1]), pack2(sl, sl), pack2(nr[-i], nr[-i - 1]));
+                            unpack2(x, s[i], s[i + 1]);
+                        }
                         sl = 1.f;
                     }
-                    if (__any_sync(0xffffffffu, lim < 128)) {
+                    if (j >= whole) {      // (a row of the warp does not see the whole tile)
 #pragma unroll
                         for (int i = 0; i < 128; ++i) s[i] = i < lim ? s[i] : -INFINITY;
                     }
@@ -167,20 +172,24 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                         }
                     }
                     const float cm = m == -INFINITY ? 0.f : c - m;      // (no key so far: exp2(-inf) = 0)
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    f2 sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         uint32_t p[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            const float p0 = exp2f(fmaf(s[64 * half + 2 * i], sl, cm)), p1 = exp2f(fmaf(s[64 * half + 2 * i + 1], sl, cm));
-                            sum[(2 * i) & 3] += p0;
-                            sum[(2 * i + 1) & 3] += p1;
+                            float p0, p1;
+                            unpack2(fma2(pack2(s[64 * half + 2 * i], s[64 * half + 2 * i + 1]), pack2(sl, sl), pack2(cm, cm)), p0, p1);
+                            p0 = exp2f(p0);
+                            p1 = exp2f(p1);
+                            sum[i & 1] = add2(sum[i & 1], pack2(p0, p1));
                             p[i] = pack_bf16(p0, p1);
                         }
                         tmem_st32(tm_s + 32u * half, p);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    float sum0, sum1;
+                    unpack2(add2(sum[0], sum[1]), sum0, sum1);
+                    l += sum0 + sum1;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&p_ready[w]);
@@ -270,66 +279,64 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
             const uint32_t id_s = idesc_bf16(128, false, false), id_o = idesc_bf16(D, false, true);
             const uint64_t d_q = smem_desc(smem_u32(sQ), 0, 1024), d_k = smem_desc(smem_u32(sK), 0, 1024), d_v = smem_desc(smem_u32(sV), SUB, 1024);
             const uint32_t q_hi = (uint32_t)(d_q >> 32), k_hi = (uint32_t)(d_k >> 32), v_hi = (uint32_t)(d_v >> 32);
-            auto issue_s = [&](int w, int s) {
+            const uint32_t leader = elect_one() ? 1u : 0u;
+            // (TMEM is allocated whole, its addresses begin at 0)
+            auto issue_s = [&](uint32_t w, uint32_t s) {
                 const uint32_t q_lo = (uint32_t)d_q + w * (TILE >> 4), k_lo = (uint32_t)d_k + s * (TILE >> 4);
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                    mma_ss_w(tmem + 128u * w, q_lo + (kk >> 2) * (SUB >> 4) + 2 * (kk & 3), q_hi, k_lo + (kk >> 2) * (SUB >> 4) + 2 * (kk & 3), k_hi, id_s, kk > 0);
-                mma_commit(&s_full[w]);
+                for (uint32_t kk = 0; kk < D / 16; ++kk)
+                    mma_ss_p(leader, 128u * w, q_lo + (kk >> 2) * (SUB >> 4) + 2u * (kk & 3u), q_hi, k_lo + (kk >> 2) * (SUB >> 4) + 2u * (kk & 3u), k_hi, id_s, kk > 0);
+                mma_commit_p(leader, &s_full[w]);
             };
-            auto issue_o = [&](int w, int s, uint32_t acc) {
+            auto issue_o = [&](uint32_t w, uint32_t s, uint32_t acc) {
                 const uint32_t v_lo = (uint32_t)d_v + s * (TILE >> 4);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) mma_ts_w(tmem + TM_O + D * w, tmem + 128u * w + 8u * kk, v_lo + 128 * kk, v_hi, id_o, acc | (kk > 0));
+                for (uint32_t kk = 0; kk < 8; ++kk) mma_ts_p(leader, TM_O + D * w, 128u * w + 8u * kk, v_lo + 128u * kk, v_hi, id_o, acc | (kk > 0));
             };
-            int uq[2] = {0, 0}, np[2] = {0, 0}, kt = 0;
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            auto wait = [&](uint64_t *bar, uint32_t parity, int site) {      // (the whole warp knows whether it ended well)
+                HDT_WAIT(bar, parity, site);
+                return HDT_AGREE();
+            };
+            uint32_t uq[2] = {0, 0}, np[2] = {0, 0}, st = 0, round = 0;      // ring stage of this tile and parity of its use
+            bool go = true;
+            for (int u = blockIdx.x; u < n_units && go; u += gridDim.x) {
                 const SelfBlk b = a.q.blk[u / H];
-                const int nt[2] = {key_tiles(b, 0), key_tiles(b, 1)}, n = max(nt[0], nt[1]);
+                const int nt[2] = {__shfl_sync(0xffffffffu, key_tiles(b, 0), 0), __shfl_sync(0xffffffffu, key_tiles(b, 1), 0)}, n = max(nt[0], nt[1]);
                 if (n == 0) continue;
-                HDT_WAIT(&k_full[kt % ST], (kt / ST) & 1, 5);
+                go = wait(&k_full[st], round, 5);
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (nt[w] > 0) {
-                        HDT_WAIT(&q_full[w], uq[w] & 1, 6);
+                for (uint32_t w = 0; w < 2; ++w)
+                    if (go && nt[w] > 0) {
+                        go = wait(&q_full[w], uq[w] & 1u, 6);
                         ++uq[w];
-                        if (!HDT_AGREE()) break;
-                        if (elect_one()) {
-                            tc_fence_after();
-                            issue_s(w, kt % ST);
-                            if (nt[w] == 1) mma_commit(&q_empty[w]);
-                        }
-                        __syncwarp();
+                        if (!go) break;
+                        tc_fence_after();
+                        issue_s(w, st);
+                        if (nt[w] == 1) mma_commit_p(leader, &q_empty[w]);
                     }
-                if (!HDT_AGREE()) break;
-                if (elect_one()) mma_commit(&k_empty[kt % ST]);
-                __syncwarp();
-                for (int j = 0; j < n && ok; ++j, ++kt) {
-                    const int s = kt % ST, s1 = (kt + 1) % ST;
-                    HDT_WAIT(&v_full[s], (kt / ST) & 1, 7);
-                    if (j + 1 < n) HDT_WAIT(&k_full[s1], ((kt + 1) / ST) & 1, 8);
+                if (!go) break;
+                mma_commit_p(leader, &k_empty[st]);
+                for (int j = 0; j < n && go; ++j) {
+                    const uint32_t s1 = st + 1 == ST ? 0 : st + 1, round1 = st + 1 == ST ? round ^ 1u : round;
+                    go = wait(&v_full[st], round, 7) && (j + 1 >= n || wait(&k_full[s1], round1, 8));
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
-                        if (j < nt[w]) {
-                            HDT_WAIT(&p_ready[w], np[w] & 1, 9);
+                    for (uint32_t w = 0; w < 2; ++w)
+                        if (go && j < nt[w]) {
+                            go = wait(&p_ready[w], np[w] & 1u, 9);
                             ++np[w];
-                            if (!HDT_AGREE()) break;
-                            if (elect_one()) {
-                                tc_fence_after();
-                                issue_o(w, s, j > 0 ? 1u : 0u);
-                                if (j + 1 < nt[w]) {
-                                    issue_s(w, s1);      // (over P, which the products before it have read)
-                                    if (j + 2 == nt[w]) mma_commit(&q_empty[w]);
-                                } else mma_commit(&o_full[w]);
-                            }
-                            __syncwarp();
+                            if (!go) break;
+                            tc_fence_after();
+                            issue_o(w, st, j > 0 ? 1u : 0u);
+                            if (j + 1 < nt[w]) {
+                                issue_s(w, s1);      // (over P, which the products before it have read)
+                                if (j + 2 == nt[w]) mma_commit_p(leader, &q_empty[w]);
+                            } else mma_commit_p(leader, &o_full[w]);
                         }
-                    if (!HDT_AGREE()) break;
-                    if (elect_one()) {
-                        mma_commit(&v_empty[s]);
-                        if (j + 1 < n) mma_commit(&k_empty[s1]);
-                    }
-                    __syncwarp();
+                    if (!go) break;
+                    mma_commit_p(leader, &v_empty[st]);
+                    if (j + 1 < n) mma_commit_p(leader, &k_empty[s1]);
+                    st = s1;
+                    round = round1;
                 }
             }
         }
