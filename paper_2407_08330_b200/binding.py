@@ -370,7 +370,7 @@ def _here(*tensors):
     """The tensors of a call are contiguous and on the current device, whose current stream the call goes to."""
     dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.device.index == dev and t.is_contiguous()):
+        if t is not None and (t.get_device() != dev or not t.is_contiguous()):      # (get_device: -1 on the CPU)
             raise HdtError(-1, "every tensor must be contiguous and on the current CUDA device")
 
 
@@ -406,9 +406,9 @@ def hdt_dropout(x, p, rng, site=0, residual=None, out=None):
     rows, cols, dt = _rows(x)
     if rng is None:
         raise HdtError(-1, "hdt_dropout: p > 0 needs the generator's state")
+    _here(x, residual, out)
+    _like(x, residual, out)
     y = torch.empty_like(x) if out is None else out
-    _here(x, residual, y)
-    _like(x, residual, y)
     rc = (_lib or lib()).hdt_dropout(x.data_ptr(), _ptr(residual), _rng(rng, p), int(site), rows, cols, dt, float(p), y.data_ptr(), _stream())
     if rc:
         _check(rc)
@@ -425,17 +425,19 @@ def hdt_layer_norm_fwd(x, weight, bias, eps=1e-5, residual=None, p=0.0, rng=None
     """h = residual + D o x, y = layer norm of h over the last dimension.  Returns (y, h, mean, rstd); h is x itself
     without a residual and without dropout."""
     rows, cols, dt = _rows(x)
-    y = torch.empty_like(x) if out is None else out
-    changed = residual is not None or p > 0
-    if h is None and changed:
-        h = torch.empty_like(x)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
-    _here(x, residual, y, h, mean, rstd, weight, bias)
-    _like(x, residual, y, h)
+    _here(x, residual, out, h, mean, rstd, weight, bias)
+    _like(x, residual, out, h)
     _norm_weights(cols, weight, bias)
-    if mean.numel() != rows or rstd.numel() != rows or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
-        raise HdtError(-1, "mean and rstd must be float32, one element per row")
+    for t in (mean, rstd):
+        if t is not None and (t.numel() != rows or t.dtype != torch.float32):
+            raise HdtError(-1, "mean and rstd must be float32, one element per row")
+    y = torch.empty_like(x) if out is None else out
+    if h is None and (residual is not None or p > 0):
+        h = torch.empty_like(x)
+    if mean is None:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty_like(mean)
     rc = (_lib or lib()).hdt_layer_norm_fwd(x.data_ptr(), _ptr(residual), weight.data_ptr(), bias.data_ptr(), _rng(rng, p), int(site), float(p), rows, cols, dt,
                                             _DTYPES[weight.dtype], float(eps), _ptr(h), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream())
     if rc:
@@ -453,6 +455,9 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
     """Gradients (d_x, d_residual, d_weight, d_bias) of hdt_layer_norm_fwd; d_h is the gradient that h gets from elsewhere.
     Without dropout d_x and d_residual are one tensor."""
     rows, cols, dt = _rows(h)
+    _here(d_y, d_h, h, d_residual, d_x, mean, rstd, weight, d_weight, d_bias, workspace)
+    _like(h, d_y, d_h, d_residual, d_x)
+    _norm_weights(cols, weight, *(t for t in (d_weight, d_bias) if t is not None))
     d_residual = torch.empty_like(h) if d_residual is None else d_residual
     if p > 0 and d_x is None:
         d_x = torch.empty_like(h)
@@ -460,9 +465,6 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
     d_bias = torch.empty_like(weight) if d_bias is None else d_bias
     if workspace is None:
         workspace = torch.empty(max(hdt_layer_norm_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=h.device)
-    _here(d_y, d_h, h, d_residual, d_x, mean, rstd, weight, d_weight, d_bias, workspace)
-    _like(h, d_y, d_h, d_residual, d_x)
-    _norm_weights(cols, weight, d_weight, d_bias)
     if mean.numel() != rows or rstd.numel() != rows or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
         raise HdtError(-1, "mean and rstd must be float32, one element per row")
     rc = (_lib or lib()).hdt_layer_norm_bwd(d_y.data_ptr(), _ptr(d_h), h.data_ptr(), mean.data_ptr(), rstd.data_ptr(), weight.data_ptr(), _rng(rng, p), int(site),
@@ -504,14 +506,14 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
     of every document), k, v [Tk,H,d]; seqlens_k [batch] where a document's part of k and v has room behind its keys (a
     cache).  Returns (O [Tq,H,d], LSE [H,Tq])."""
     B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
+    _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, out, lse, workspace)
+    _like(q, out)
+    if lse is not None and (lse.shape != (H, Tq) or lse.dtype != torch.float32):
+        raise HdtError(-1, "lse must be float32 [heads, rows of q]")
     out = torch.empty_like(q) if out is None else out
     lse = torch.empty((H, Tq), dtype=torch.float32, device=q.device) if lse is None else lse
     if workspace is None:
         workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, False)), dtype=torch.uint8, device=q.device)
-    _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, out, lse, workspace)
-    _like(q, out)
-    if lse.shape != (H, Tq) or lse.dtype != torch.float32:
-        raise HdtError(-1, "lse must be float32 [heads, rows of q]")
     rc = (_lib or lib()).hdt_self_attn_fwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                            _ptr(bias), n, int(max_distance), int(bool(causal)), out.data_ptr(), lse.data_ptr(), H, d, _DTYPES[q.dtype],
                                            float(softmax_scale), workspace.data_ptr(), workspace.numel(), _stream())
@@ -524,13 +526,6 @@ def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=Non
                       dq=None, dk=None, dv=None, d_bias=None, workspace=None):
     """Gradients (dQ, dK, dV, dBias) of hdt_self_attn_fwd; dBias is None without a bias."""
     B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(k) if dv is None else dv
-    if bias is not None and d_bias is None:
-        d_bias = torch.empty_like(bias)
-    if workspace is None:
-        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, True)), dtype=torch.uint8, device=q.device)
     _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, o, lse, d_o, dq, dk, dv, d_bias, workspace)
     _like(q, o, d_o, dq)
     _like(k, dk, dv)
@@ -538,6 +533,13 @@ def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=Non
         _like(bias, d_bias)
     if lse.shape != (H, Tq) or lse.dtype != torch.float32:
         raise HdtError(-1, "lse must be float32 [heads, rows of q]")
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(k) if dv is None else dv
+    if bias is not None and d_bias is None:
+        d_bias = torch.empty_like(bias)
+    if workspace is None:
+        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, True)), dtype=torch.uint8, device=q.device)
     rc = (_lib or lib()).hdt_self_attn_bwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                            _ptr(bias), n, int(max_distance), int(bool(causal)), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(), dq.data_ptr(),
                                            dk.data_ptr(), dv.data_ptr(), _ptr(d_bias), H, d, _DTYPES[q.dtype], float(softmax_scale), workspace.data_ptr(),

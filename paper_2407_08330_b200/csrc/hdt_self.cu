@@ -75,6 +75,7 @@ __device__ __forceinline__ int scan1024(int v, int *s_warp) {
 __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ PrepArgs a) {
     constexpr int BINS = 1024;
     __shared__ int s_warp[32], s_pre[1024], s_bin[BINS];
+    __shared__ Doc s_doc[1024];
     const int t = threadIdx.x;
     pdl_launch_dependents();
     if ((int)blockIdx.x >= a.n_lists) {      // the bias by distance
@@ -88,10 +89,13 @@ __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ Prep
     const PrepList L = a.list[blockIdx.x];
     s_bin[t] = 0;
     int total = 0;
+    SelfBlk mine{};      // block number t, where this thread comes to it, stays in registers; the others take the way through `raw`
+    bool have = false;
     for (int b0 = 0; b0 < a.B; b0 += 1024) {
         int nb = 0;
         if (b0 + t < a.B) {
             const Doc d = document(a.cu_q, a.cu_k, a.len_k, b0 + t, a.Tq, a.Tk);
+            s_doc[t] = d;
             nb = ((L.of_keys ? d.nk : d.nq) + L.rows - 1) / L.rows;
         }
         s_pre[t] = scan1024(nb, s_warp);
@@ -104,26 +108,29 @@ __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ Prep
                 if (s_pre[mid] > i) hi = mid;
                 else lo = mid + 1;
             }
-            const Doc d = document(a.cu_q, a.cu_k, a.len_k, b0 + lo, a.Tq, a.Tk);
+            const Doc d = s_doc[lo];
             SelfBlk x;
             x.q0 = d.q0; x.nq = d.nq; x.k0 = d.k0; x.nk = d.nk; x.off = d.nk - d.nq;
             x.r0 = (i - (lo > 0 ? s_pre[lo - 1] : 0)) * L.rows;
             x.tiles = L.of_keys ? (d.nq - self_first_row(a.rel.causal, x.r0, d.nq, d.nk) + 127) >> 7 : (self_keys_of(a.rel.causal, x.r0, L.rows, d.nq, d.nk) + 127) >> 7;
             x.id = total + i;
             if (x.id >= L.most) break;       // (documents that overlap: there is room for those that do not)
-            L.raw[x.id] = x;
+            if (x.id == t) {
+                mine = x;
+                have = true;
+            } else L.raw[x.id] = x;
             atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1);
         }
         total += n;
         __syncthreads();
     }
     total = min(total, L.most);
-    const int mine = s_bin[t];
-    const int start = scan1024(mine, s_warp) - mine;      // (its barriers lie between the last read and the next write)
+    const int n_bin = s_bin[t];
+    const int start = scan1024(n_bin, s_warp) - n_bin;      // (its barriers lie between the last read and the next write)
     s_bin[t] = start;
     __syncthreads();
     for (int i = t; i < total; i += 1024) {
-        const SelfBlk x = L.raw[i];
+        const SelfBlk x = i == t && have ? mine : L.raw[i];
         L.out[atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1)] = x;
     }
     if (t == 0) *L.count = total;
