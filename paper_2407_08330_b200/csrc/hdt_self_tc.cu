@@ -33,13 +33,18 @@ template <int D>
 struct FwdShape {
     static constexpr int ST = D == 64 ? 3 : 2, TILE = SUB * (D / 64), NS = D / 64;
     static constexpr int SMEM = (2 + 2 * ST) * TILE + 4 * 256 * 4 + 256;
+    // At head_dim 128 the bias vector of the next near tile is requested a tile ahead, and the softmax warps have the registers for
+    // it (4 x 4096 tokens 309 -> 295 us, borders up to 2000 340 -> 318).  At 64, where the two row tiles' exponentials
+    // have to take turns, the same slows far tiles (1 x 16384 both ways 1237 -> 1308 us, 16 x 512 36.5 -> 34.2).
+    static constexpr bool NEAR_AHEAD = D == 128;
 };
 }  // namespace
 
 template <int D>
 __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                                                      const __grid_constant__ CUtensorMap tm_v, const SelfFwdArgs a) {
-    constexpr int ST = FwdShape<D>::ST, TILE = FwdShape<D>::TILE, NS = FwdShape<D>::NS;
+    using Sh = FwdShape<D>;
+    constexpr int ST = Sh::ST, TILE = Sh::TILE, NS = Sh::NS;
     constexpr uint32_t TM_O = 256, TM_COLS = 512;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *sQ = smem_raw, *sK = sQ + 2 * TILE, *sV = sK + ST * TILE;
@@ -97,9 +102,10 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
     };
 
     // 168 registers a thread at launch (384 threads): the softmax warps take what the others do not need
-    // (256 x 208 + 128 x 88 = 384 x 168)
+    // (256 x 208 + 128 x 88 = 384 x 168, or 256 x 224 + 128 x 56)
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        if constexpr (D == 64) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         if (!dead) {
             // ================= softmax: row tile w, a thread per row =================
             const int w = warp >> 2, rl = tid & 127;
@@ -113,7 +119,11 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                 const int lim0 = !valid ? 0 : a.causal ? min(max(b.off + row + 1, 0), b.nk) : b.nk;
                 const float *bias = a.dist.bias + (size_t)h * a.dist.n;
                 const int whole = __reduce_min_sync(0xffffffffu, lim0) >> 7;      // tiles that every row of the warp sees whole
-                float m = -INFINITY, l = 0.f;
+                float m = -INFINITY, l = 0.f, ahead[2] = {0.f, 0.f};
+                auto request_near = [&](int base) {      // this thread's two entries of a tile's bias vector
+                    ahead[0] = bias[self_dist_at(a.dist, base + rl - 127)];
+                    ahead[1] = bias[self_dist_at(a.dist, base + rl + 1)];
+                };
                 for (int j = 0; j < nt; ++j, ++ns) {
                     const int base = first - 128 * j, lim = lim0 - 128 * j;
                     float c = 0.f;
@@ -124,9 +134,13 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                         else if (base + 127 <= -a.dist.far) c = bias[0];
                         else {
                             near = true;
-                            nb[rl] = bias[self_dist_at(a.dist, base + rl - 127)];
-                            nb[rl + 128] = bias[self_dist_at(a.dist, base + rl + 1)];
+                            if (!Sh::NEAR_AHEAD || j == 0) request_near(base);
+                            nb[rl] = ahead[0];
+                            nb[rl + 128] = ahead[1];
                             mbar_arrive(&nb_full[w]);      // (an mbarrier, whose wait is bounded, and not a CTA barrier)
+                        }
+                        if (Sh::NEAR_AHEAD && j + 1 < nt && base - 128 - 127 < a.dist.far && base - 128 + 127 > -a.dist.far) request_near(base - 128);
+                        if (near) {
                             HDT_WAIT(&nb_full[w], near_no & 1, 12);
                             ++near_no;
                         }
@@ -227,7 +241,8 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if constexpr (D == 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (dead) {
         } else if (warp == 8) {
             // ================= load warp =================

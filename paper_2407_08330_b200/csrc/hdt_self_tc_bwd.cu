@@ -26,7 +26,7 @@
 // What bounds it is the tensor pipe's operand reads: a product of M = 128, N = 64, K = 16 takes about 75 cycles with both
 // operands in shared memory and 40 with A in TMEM.  So at head_dim 64 the resident tiles lie in TMEM too.
 // TMEM: S of either step 64 columns (P over it), dP 64 (dS over it), the accumulators 2 x 64 or 2 x 128, at head_dim 64 the
-// resident tiles 2 x 32.  One buffer of each is enough: S of a step's next tile is computed, behind the product that reads P,
+// resident tiles of two units, 2 x 32 each.  One buffer of each is enough: S of a step's next tile is computed, behind the product that reads P,
 // while the compute warps are at dS, and dP, behind the one that reads dS, while they are at the next P.
 //
 // Rows that are not the document's (the walked tile's tail) are set to zero in shared memory: their P and dS are 0, but
@@ -150,9 +150,9 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
     float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: [4][128] row sums of dS; keys: per compute warp [buckets] and [32] of scratch
     uint64_t *bars = (uint64_t *)((uint8_t *)sSum + Sh::SUMS);
     // resident tiles: loaded, free, in TMEM, read for the last time; walked tiles; S, dP; P, dS; accumulators; the rest
-    uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 3, *s_full = bars + 4, *dp_full = bars + 6, *p_ready = bars + 8, *ds_ready = bars + 10;
-    uint64_t *acc_full = bars + 12, *acc_free = bars + 13, *fix = bars + 14, *sum_full = bars + 15, *sum_free = bars + 16;
-    uint64_t *t_full = bars + 17, *t_empty = t_full + ST;
+    uint64_t *r_full = bars, *r_empty = bars + 1, *r_ready = bars + 2, *r_free = bars + 4, *s_full = bars + 6, *dp_full = bars + 8, *p_ready = bars + 10, *ds_ready = bars + 12;
+    uint64_t *acc_full = bars + 14, *acc_free = bars + 15, *fix = bars + 16, *sum_full = bars + 17, *sum_free = bars + 18;
+    uint64_t *t_full = bars + 19, *t_empty = t_full + ST;
     uint32_t *slot = (uint32_t *)(t_empty + ST);
     volatile int *abort_flag = (volatile int *)(slot + 1);
 
@@ -165,9 +165,9 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
     if (tid == 0) {
         mbar_init(r_full, 1);
         mbar_init(r_empty, RTM ? 128 : 1);
-        mbar_init(r_ready, 128);
-        mbar_init(r_free, 1);
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&r_ready[i], 128);
+            mbar_init(&r_free[i], 1);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[i], 256);
             mbar_init(&dp_full[i], 1);
@@ -511,12 +511,12 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             const uint32_t r_hi = (uint32_t)(d_r >> 32), sk_hi = (uint32_t)(d_sk >> 32), sm_hi = (uint32_t)(d_sm >> 32);
             constexpr uint32_t T16 = TILE >> 4, S16 = SUB >> 4;
             // (TMEM is allocated whole, its addresses begin at 0)
-            auto issue_sdp = [&](uint32_t q, uint32_t dst, uint32_t x, uint32_t s) {      // S (q = 0) or dP (1) of columns 64 x ..
+            auto issue_sdp = [&](uint32_t q, uint32_t dst, uint32_t x, uint32_t s, uint32_t rb) {      // S (q = 0) or dP (1) of columns 64 x ..
                 const uint32_t r_lo = (uint32_t)d_r + q * T16, s_lo = (uint32_t)d_sk + (s * 2u + q) * T16 + x * (8192u >> 4);
 #pragma unroll
                 for (uint32_t kk = 0; kk < D / 16; ++kk) {
                     const uint32_t o = (kk >> 2) * S16 + 2u * (kk & 3u);
-                    if (RTM) mma_ts_p(leader, dst, TM_R + 32u * q + 8u * kk, s_lo + o, sk_hi, id_s, kk > 0);
+                    if (RTM) mma_ts_p(leader, dst, TM_R + 64u * rb + 32u * q + 8u * kk, s_lo + o, sk_hi, id_s, kk > 0);
                     else mma_ss_p(leader, dst, r_lo + o, r_hi, s_lo + o, sk_hi, id_s, kk > 0);
                 }
             };
@@ -539,58 +539,66 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             };
             int nt = next_nt(), nt_n = nt > 0 ? next_nt() : 0, j = 0;
             uint32_t uc = 0, st = 0, tp = 0, par = 0;      // unit; ring stage of this tile and parity of its use; parity of the tile number
-            auto put_s = [&](uint32_t x, uint32_t s_) {
-                issue_sdp(0, TM_S + 64u * x, x, s_);
+            // rb: which of the two units in TMEM (head_dim 64)
+            auto put_s = [&](uint32_t x, uint32_t s_, uint32_t rb) {
+                issue_sdp(0, TM_S + 64u * x, x, s_, rb);
                 mma_commit_p(leader, &s_full[x]);
             };
-            auto put_dp = [&](uint32_t x, uint32_t s_, bool last_of_unit) {
-                issue_sdp(1, TM_P + 64u * x, x, s_);
+            auto put_dp = [&](uint32_t x, uint32_t s_, uint32_t rb, bool last_of_unit) {
+                issue_sdp(1, TM_P + 64u * x, x, s_, rb);
                 mma_commit_p(leader, &dp_full[x]);
-                if (x == 1 && last_of_unit) mma_commit_p(leader, RTM ? r_free : r_empty);      // the last that reads the resident tiles
+                if (x == 1 && last_of_unit) mma_commit_p(leader, RTM ? &r_free[rb] : r_empty);      // the last that reads the resident tiles
             };
-            bool go = nt > 0 && wait(RTM ? r_ready : r_full, 0, 4) && wait(&t_full[0], 0, 5);
+            auto resident = [&](uint32_t unit_no) {      // the unit's resident tiles are there
+                return RTM ? wait(&r_ready[unit_no & 1u], (unit_no >> 1) & 1u, 4) : wait(r_full, unit_no & 1u, 4);
+            };
+            bool go = nt > 0 && resident(0) && wait(&t_full[0], 0, 5);
             if (go) {
                 tc_fence_after();
-                put_s(0, 0);
-                put_s(1, 0);
-                put_dp(0, 0, false);
-                put_dp(1, 0, nt == 1);
+                put_s(0, 0, 0);
+                put_s(1, 0, 0);
+                put_dp(0, 0, 0, false);
+                put_dp(1, 0, 0, nt == 1);
             }
             while (go && nt > 0) {
-                const bool last = j + 1 == nt, opens = last && nt_n > 0;      // the next tile opens a unit
-                const uint32_t s1 = st + 1 == ST ? 0 : st + 1, tp1 = st + 1 == ST ? tp ^ 1u : tp, acc = j == 0 ? 0u : 1u;
-                if (j == 0 && uc > 0 && !wait(acc_free, (uc - 1) & 1u, 6)) break;
+                const bool last = j + 1 == nt, opens = last && nt_n > 0, more = !last || opens;      // the next tile: opens a unit, is there
+                const bool last1 = last ? nt_n == 1 : j + 2 == nt;                                      // is its unit's last
+                // resident tiles in shared memory, one buffer: the next unit's come when this unit's last S and dP are through
+                const bool defer = !RTM && opens;
+                const uint32_t s1 = st + 1 == ST ? 0 : st + 1, tp1 = st + 1 == ST ? tp ^ 1u : tp, acc = j == 0 ? 0u : 1u, rb1 = (uc + (last ? 1u : 0u)) & 1u;
 #pragma unroll
                 for (uint32_t x = 0; x < 2; ++x) {
                     go = wait(&p_ready[x], par, 7);
+                    if (go && x == 0 && j == 0 && uc > 0) go = wait(acc_free, (uc - 1) & 1u, 6);
                     if (!go) break;
                     tc_fence_after();
                     issue_acc(TM_ACC + D, TM_S + 64u * x, ROWS ? 0 : 1, x, st, x == 0 ? acc : 1u);
-                    if (!last) {
+                    if (more && !defer) {
                         if (x == 0) {
-                            go = wait(&t_full[s1], tp1, 5);
+                            go = (!opens || resident(uc + 1)) && wait(&t_full[s1], tp1, 5);
                             if (!go) break;
+                            tc_fence_after();
                         }
-                        put_s(x, s1);
+                        put_s(x, s1, rb1);
                     }
                     go = wait(&ds_ready[x], par, 8);
                     if (!go) break;
                     tc_fence_after();
                     issue_acc(TM_ACC, TM_P + 64u * x, 0, x, st, x == 0 ? acc : 1u);
                     if (x == 1) mma_commit_p(leader, &t_empty[st]);
-                    if (!last) put_dp(x, s1, j + 2 == nt);
+                    if (more && !defer) put_dp(x, s1, rb1, last1);
                 }
                 if (!go) break;
                 if (last) {
                     mma_commit_p(leader, acc_full);
-                    if (opens) {      // the next unit's resident tiles come behind this unit's last S and dP
-                        go = wait(RTM ? r_ready : r_full, (uc + 1) & 1u, 4) && wait(&t_full[s1], tp1, 5);
+                    if (defer) {
+                        go = resident(uc + 1) && wait(&t_full[s1], tp1, 5);
                         if (!go) break;
                         tc_fence_after();
-                        put_s(0, s1);
-                        put_s(1, s1);
-                        put_dp(0, s1, false);
-                        put_dp(1, s1, nt_n == 1);
+                        put_s(0, s1, 0);
+                        put_s(1, s1, 0);
+                        put_dp(0, s1, 0, false);
+                        put_dp(1, s1, 0, last1);
                     }
                     nt = nt_n;
                     nt_n = nt > 0 ? next_nt() : 0;
@@ -606,7 +614,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             const int rl = tid & 127;
             int uc = 0, um = 0, u_move = blockIdx.x;
             // the resident tiles of the next unit that has any: from shared memory into TMEM, once the last products with those
-            // before them are through
+            // of two units before are through
             auto move_next = [&]() {
                 if (!RTM) return;
                 for (; u_move < n_units && unit(u_move).nt == 0; u_move += gridDim.x) {}
@@ -614,7 +622,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                 u_move += gridDim.x;
                 const uint8_t *r = sR + (um % RES) * 2 * TILE;
                 HDT_WAIT(&r_full[um % RES], (um / RES) & 1, 16);
-                if (um > 0) HDT_WAIT(r_free, (um - 1) & 1, 17);
+                if (um > 1) HDT_WAIT(&r_free[um & 1], ((um >> 1) - 1) & 1, 17);
                 if (!HDT_AGREE()) return;
                 tc_fence_after();
 #pragma unroll
@@ -625,18 +633,18 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                         const uint4 z = *reinterpret_cast<const uint4 *>(r + (q >> 1) * TILE + swz(rl, 4 * (q & 1) + e));
                         y[4 * e] = z.x; y[4 * e + 1] = z.y; y[4 * e + 2] = z.z; y[4 * e + 3] = z.w;
                     }
-                    tmem_st16(tmem + TM_R + 16u * q + lane_base, y);
+                    tmem_st16(tmem + TM_R + 64u * (um & 1) + 16u * q + lane_base, y);
                 }
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(&r_empty[um % RES]);
-                mbar_arrive(r_ready);
+                mbar_arrive(&r_ready[um & 1]);
                 ++um;
             };
             move_next();
+            move_next();
             for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
                 const Unit U = unit(u);
-                if (U.nt > 0) move_next();
                 const int nrows = min(128, (ROWS ? U.b.nq : U.b.nk) - U.b.r0);
                 float r = 0.f;
                 if (U.nt > 0) HDT_WAIT(sum_full, uc & 1, 13);
@@ -705,6 +713,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     }
                     group_all(true, 1, 128);      // (the staging tile has been read)
                 }
+                if (U.nt > 0) move_next();      // (the unit after the next, where this one's was)
             }
             if (rl == 0) bulk_wait_all();
         }
