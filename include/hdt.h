@@ -316,7 +316,7 @@ int hdt_cross_attn_bwd(const int8_t *level, const int32_t *cu_seqlens_k, const i
  *                      at every replay once its caller has advanced the offset
  *   site               tells the dropouts of one network apart that share a state
  *   p                  in [0, 1)
- * rows < 2^31 - 255, 1 <= cols <= 8192.  Rows whose length is a multiple of 8 in tensors that are 16-byte aligned are the fast
+ * rows <= 2^31 - 2^16, 1 <= cols <= 8192.  Rows whose length is a multiple of 8 in tensors that are 16-byte aligned are the fast
  * case; any other alignment to the element works.  Arithmetic in fp32, rounded once.  Asynchronous on `stream`.
  */
 int hdt_dropout(const void *x, const void *residual, const int64_t *rng, int32_t site, int64_t rows, int32_t cols,

@@ -208,10 +208,8 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : WP
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[i][e] = fmaf(g[i][e] - m1 - x[i][e] * m2, rstd, a.dh != nullptr ? y[e] : 0.f);
             if (on) store8<LPR, VEC>((T *)a.dres + at, w0 + i * WPR, l, a.cols, g[i]);
-            if (a.drop.rng != nullptr) {
-                drop8<LPR, VEC>(key, a.drop, row, w0 + i * WPR, l, g[i]);
-                if (on) store8<LPR, VEC>((T *)a.dx + at, w0 + i * WPR, l, a.cols, g[i]);
-            }
+            if (a.drop.rng != nullptr) drop8<LPR, VEC>(key, a.drop, row, w0 + i * WPR, l, g[i]);
+            if (a.dx != nullptr && on) store8<LPR, VEC>((T *)a.dx + at, w0 + i * WPR, l, a.cols, g[i]);
         }
     }
     // the CTA's column sums: over the row groups of a warp by shuffles, over the warps through shared memory
@@ -319,7 +317,7 @@ int make_drop(Drop *d, const int64_t *rng, int32_t site, float p, bool wanted, c
 
 int norm_check(int64_t rows, int32_t cols, int32_t dtype, int32_t w_dtype, const char *who) {
     if (rows < 0 || cols < 1) return set_error(HDT_ERR_INVALID_ARG, "%s: negative number of rows or no column", who);
-    if (rows > 0x7fffff00LL || cols > 8192) return set_error(HDT_ERR_UNSUPPORTED, "%s: at most 2^31 - 256 rows and 8192 columns", who);
+    if (rows > 0x7fff0000LL || cols > 8192) return set_error(HDT_ERR_UNSUPPORTED, "%s: at most 2^31 - 2^16 rows and 8192 columns", who);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (w_dtype != HDT_F32 && w_dtype != dtype) return set_error(HDT_ERR_UNSUPPORTED, "%s: weights must be fp32 or of the rows' type", who);
     return HDT_OK;
@@ -437,7 +435,7 @@ extern "C" int hdt_layer_norm_fwd(const void *x, const void *residual, const voi
     if (const int rc = make_drop(&a.drop, rng, site, p, false, "hdt_layer_norm_fwd")) return rc;
     if (rows == 0) return HDT_OK;
     if (!x || !weight || !bias || !y || !mean || !rstd) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_fwd: null tensor pointer");
-    if (!h && (residual || a.drop.rng)) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_fwd: with a residual or dropout h has to be written");
+    if (!h && (residual || p > 0.f)) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_fwd: with a residual or dropout h has to be written");
     const uintptr_t el = dtype == HDT_F32 ? 3 : 1, wl = w_dtype == HDT_F32 ? 3 : 1;
     if ((((uintptr_t)x | (uintptr_t)residual | (uintptr_t)h | (uintptr_t)y) & el) || (((uintptr_t)weight | (uintptr_t)bias) & wl) ||
         (((uintptr_t)mean | (uintptr_t)rstd) & 3))
@@ -449,7 +447,7 @@ extern "C" int hdt_layer_norm_fwd(const void *x, const void *residual, const voi
 }
 
 extern "C" size_t hdt_layer_norm_workspace_bytes(int64_t rows, int32_t cols) {
-    if (rows < 0 || rows > 0x7fffff00LL || cols < 1 || cols > 8192) return 0;
+    if (rows < 0 || rows > 0x7fff0000LL || cols < 1 || cols > 8192) return 0;
     const int g = bwd_grid(rows, cols);
     return ((size_t)(g > 0 ? g : 1) * 2 * cols * 4 + 255) / 256 * 256;
 }
@@ -461,7 +459,7 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
     NormArgs a{};
     if (const int rc = make_drop(&a.drop, rng, site, p, false, "hdt_layer_norm_bwd")) return rc;
     if (!d_weight || !d_bias) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: null tensor pointer");
-    if (rows > 0 && (!d_y || !h || !mean || !rstd || !weight || !d_residual || (a.drop.rng && !d_x)))
+    if (rows > 0 && (!d_y || !h || !mean || !rstd || !weight || !d_residual || (p > 0.f && !d_x)))
         return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: null tensor pointer");
     const size_t need = hdt_layer_norm_workspace_bytes(rows, cols);
     if (!workspace || workspace_bytes < need) return set_error(HDT_ERR_WORKSPACE, "hdt_layer_norm_bwd: workspace %zu < required %zu", workspace_bytes, need);
@@ -470,7 +468,8 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
     if ((((uintptr_t)d_y | (uintptr_t)d_h | (uintptr_t)h | (uintptr_t)d_residual | (uintptr_t)d_x) & el) || (((uintptr_t)weight | (uintptr_t)d_weight | (uintptr_t)d_bias) & wl) ||
         (((uintptr_t)mean | (uintptr_t)rstd) & 3))
         return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: misaligned tensor");
-    a.dy = d_y; a.dh = d_h; a.hin = h; a.mean_in = mean; a.rstd_in = rstd; a.weight = weight; a.dres = d_residual; a.dx = d_x;
+    a.dy = d_y; a.dh = d_h; a.hin = h; a.mean_in = mean; a.rstd_in = rstd; a.weight = weight; a.dres = d_residual;
+    a.dx = p > 0.f ? d_x : nullptr;      // (a p that rounds to no dropout at all has its gradient too)
     a.part = (float *)workspace; a.rows = (int)rows; a.cols = cols;
     cudaStream_t st = (cudaStream_t)stream;
     if (rows > 0) {

@@ -169,8 +169,8 @@ struct StepDoc {      // how a document's work is cut: row groups x pieces of ke
     int groups, per, pieces;
     __device__ __forceinline__ StepDoc(const Doc &d, int piece) {
         groups = (d.nq + RG - 1) / RG;
-        per = piece * groups;
-        pieces = groups == 0 ? 0 : max(1, (d.nk + per - 1) / per);
+        per = (int)max(1ll, min((long long)piece * groups, (long long)d.nk));
+        pieces = groups == 0 ? 0 : max(1, d.nk / per + (d.nk % per > 0));
     }
     __device__ __forceinline__ int items() const { return groups * pieces; }
 };
@@ -460,7 +460,7 @@ int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distan
     if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7fffff00LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
-    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7fffff00LL || step_items(B, Tq, Tk, H, 1) * H > 0x7fffff00LL)
+    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7fffff00LL || step_items(B, Tq, Tk, H, 1) * H > 0x7fffff00LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fffff00LL))
         return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
     if (buckets > 0) {
         const int one = causal ? buckets : buckets / 2;

@@ -59,9 +59,9 @@ def _bwd(dy=A, h=A, mean=A, w=A, rng=None, p=0.0, rows=4, cols=8, dtype=1, w_dty
     (lambda: _drop(rng=None), -1), (lambda: _drop(rng=A + 4), -1), (lambda: _drop(x=None), -1), (lambda: _drop(y=None), -1), (lambda: _drop(x=A + 1), -1),
     (lambda: _drop(dtype=0, y=ODD), -1), (lambda: _drop(rows=0, x=None, y=None), 0),
     (lambda: _fwd(w_dtype=3), -3), (lambda: _fwd(dtype=0, w_dtype=1), -3), (lambda: _fwd(eps=-1.0), -1), (lambda: _fwd(eps=float("nan")), -1),
-    (lambda: _fwd(p=0.5), -1), (lambda: _fwd(p=0.5, rng=A), -1), (lambda: _fwd(res=A), -1), (lambda: _fwd(w=None), -1), (lambda: _fwd(mean=None), -1),
+    (lambda: _fwd(p=0.5), -1), (lambda: _fwd(p=0.5, rng=A), -1), (lambda: _fwd(p=1e-7, rng=A), -1), (lambda: _fwd(res=A), -1), (lambda: _fwd(w=None), -1), (lambda: _fwd(mean=None), -1),
     (lambda: _fwd(mean=ODD), -1), (lambda: _fwd(w_dtype=0, w=ODD), -1), (lambda: _fwd(rows=0), 0),
-    (lambda: _bwd(dy=None), -1), (lambda: _bwd(dw=None), -1), (lambda: _bwd(p=0.5, rng=A), -1), (lambda: _bwd(ws=None), -4), (lambda: _bwd(n=63), -4),
+    (lambda: _bwd(dy=None), -1), (lambda: _bwd(dw=None), -1), (lambda: _bwd(p=0.5, rng=A), -1), (lambda: _bwd(p=1e-7, rng=A), -1), (lambda: _bwd(rows=2 ** 31 - 2 ** 15), -3), (lambda: _bwd(ws=None), -4), (lambda: _bwd(n=63), -4),
     (lambda: _bwd(ws=A + 128), -1), (lambda: _bwd(h=A + 1), -1), (lambda: _bwd(cols=9000), -3),
 ])
 def test_refusals(call, code):

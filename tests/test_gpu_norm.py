@@ -137,6 +137,17 @@ def test_in_place_and_repeated_calls_give_the_same_bits():
     assert torch.equal(P.hdt_dropout(z, 0.1, rng, residual=r, out=z), P.hdt_dropout(x, 0.1, rng, residual=r))
 
 
+def test_a_p_that_rounds_to_none():
+    """p below 2^-17 drops nothing; h and the gradient of x are written all the same."""
+    import paper_2407_08330_b200 as P
+    rng, _, _ = state()
+    x, w, dy = torch.randn(5, 64, device="cuda"), torch.ones(64, device="cuda"), torch.randn(5, 64, device="cuda")
+    h, dx = torch.full_like(x, 9.0), torch.full_like(x, 9.0)
+    y, _, mean, rstd = P.hdt_layer_norm_fwd(x, w, w, p=1e-6, rng=rng, h=h)
+    got, dres, _, _ = P.hdt_layer_norm_bwd(dy, h, mean, rstd, w, p=1e-6, rng=rng, d_x=dx)
+    assert torch.equal(h, x) and got is dx and torch.equal(dx, dres) and dx is not dres
+
+
 def test_rows_of_non_finite_values_stay_to_themselves():
     import paper_2407_08330_b200 as P
     x = torch.randn(9, 200, device="cuda")
