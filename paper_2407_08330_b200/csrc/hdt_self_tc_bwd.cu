@@ -235,16 +235,27 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
             const uint32_t tm_s = tmem + TM_S + 64u * x + 32u * qh + lane_base, tm_dp = tmem + TM_P + 64u * x + 32u * qh + lane_base;
             int st = 0, tp = 0, uc = 0, par = 0;
+            auto flush = [&](float v, int at) {      // a warp's sum beyond the borders, to the bucket of distance number `at`
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if (lane == 0) sum[a.dist.bucket[at]] += v;
+                __syncwarp();
+            };
             for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
                 // (what a unit needs in its loop, and no more: p and d fill the registers)
-                int nt, base, first, end;      // tiles; distance of lane 0 and column 0; columns that this lane's row pairs with, from c0 on
+                int nt, first, end;            // tiles; columns that this lane's row pairs with, from c0 on
                 int whole0, whole1;            // tiles in which every lane of the warp keeps all its columns
-                float row_l = 0.f, row_d = 0.f, by_side[2] = {0.f, 0.f};      // rows: -LSE' and -delta'; -LSE' with the bias of either side beyond the borders
+                int near0 = 0, near1 = 0;      // tiles with distances inside the borders; those before and behind lie beyond them
+                float row_l = 0.f, row_d = 0.f, by_side[2];      // rows: -LSE' and -delta'; -LSE' with the bias of the tiles before and behind the near ones
                 {
                     const Unit U = unit(u);
                     if (U.nt == 0) continue;
                     nt = U.nt;
-                    base = base_of(U, 0);
+                    const int base = base_of(U, 0);
+                    if (a.bias_on) {
+                        near0 = max(((ROWS ? base - 127 - a.dist.far : -a.dist.far - 127 - base) >> 7) + 1, 0);
+                        near1 = max(((ROWS ? base + 127 + a.dist.far : a.dist.far + 127 - base) + 127) >> 7, near0);
+                    }
                     const int row = U.b.r0 + rl;
                     first = end = 0;
                     if (row < (ROWS ? U.b.nq : U.b.nk)) {
@@ -263,16 +274,20 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     end -= U.c0 + c0;
                     whole0 = (max(__reduce_max_sync(0xffffffffu, first), 0) + 127) >> 7;
                     whole1 = (__reduce_min_sync(0xffffffffu, end) - 32 + 128) >> 7;
-                    if (ROWS && a.bias_on) {
-                        by_side[0] = row_l + a.dist.bias[(size_t)U.h * a.dist.n];
-                        by_side[1] = row_l + a.dist.bias[(size_t)(U.h + 1) * a.dist.n - 1];
+                    by_side[0] = by_side[1] = row_l;
+                    if (ROWS && a.bias_on) {      // (keys behind the query come last)
+                        by_side[0] += a.dist.bias[(size_t)(U.h + 1) * a.dist.n - 1];
+                        by_side[1] += a.dist.bias[(size_t)U.h * a.dist.n];
                     }
                 }
-                float far_sum[2] = {0.f, 0.f};
+                float far_sum = 0.f;
                 f2 row_sum = pack2(0.f, 0.f);
                 for (int j = 0; j < nt; ++j) {
-                    const int side = far_side(base);
-                    base += ROWS ? -128 : 128;
+                    const bool near = j >= near0 && j < near1;
+                    if (sums && j == near0 && j > 0) {      // what was summed so far lies behind the query, what comes after the near tiles before it
+                        flush(far_sum, 0);
+                        far_sum = 0.f;
+                    }
                     const uint8_t *stat = sStat + st * Sh::STAT;
                     uint32_t keep = 0xffffffffu;
                     const bool all = j >= whole0 && j < whole1;
@@ -284,18 +299,18 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     }
                     first -= 128;
                     end -= 128;
-                    const float l = !ROWS || side == 0 || side == 2 ? row_l : by_side[side == 1];
+                    const float l = !ROWS || near ? row_l : by_side[j >= near1];
                     if (j == 0 && uc > 0) HDT_WAIT(sum_free, (uc - 1) & 1, 18);      // the drain group has read the last unit's sums
                     HDT_WAIT(&s_full[x], par, 12);      // (a wait that ran out changes nothing in what the warp does before the tile's end)
                     tc_fence_after();
-                    uint32_t p[32];
+                    uint32_t p[32], d2[2][16];
                     if (any) {
                         tmem_ld32(tm_s, p);
                         tmem_wait_ld();
                         const float *neg_l = reinterpret_cast<const float *>(stat) + c0;
                         // entry (row, column) of a tile with near distances: + 1 per row, - 1 per key
                         const float *n = reinterpret_cast<const float *>(stat + 1024) + 127 + (ROWS ? rl - c0 : c0 - rl);
-                        if (side == 0) {
+                        if (near) {
                             if (all) probabilities<ROWS, true, false>(p, neg_l, n, l, a.scale_log2, keep);
                             else probabilities<ROWS, true, true>(p, neg_l, n, l, a.scale_log2, keep);
                         } else if (all) probabilities<ROWS, false, false>(p, neg_l, n, l, a.scale_log2, keep);
@@ -317,7 +332,6 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     HDT_WAIT(&dp_full[x], par, 15);
                     tc_fence_after();
                     float diag = 0.f;
-                    uint32_t d2[2][16];
                     if (any && !ROWS) tmem_ld16(tm_dp, d2[0]);      // (rows: no room for a second load in flight)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -336,7 +350,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
 #pragma unroll
                         for (int e = 0; e < 8; ++e) y[e] = pack_bf16(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
                         tmem_st8(tm_dp + 8u * i, y);
-                        if (ROWS || (sums && side != 0)) {
+                        if (ROWS || (sums && !near)) {
                             f2 v = pack2(0.f, 0.f);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) v = add2(v, pack2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])));
@@ -344,7 +358,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                             else {
                                 float v0, v1;
                                 unpack2(v, v0, v1);
-                                far_sum[side == -1] += v0 + v1;
+                                far_sum += v0 + v1;
                             }
                         } else if (sums && any) {
 #pragma unroll
@@ -365,7 +379,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     // distances 31 - lane (this lane's sum) and lane - 32 (in scratch, lanes 1..31) from the piece's corner: their buckets,
                     // before the arrival that lets the load warp use the stage again
                     int bks[2] = {255, 255};
-                    if (sums && side == 0 && any) {
+                    if (sums && near && any) {
                         const uint8_t *at = stat + 2048 + 127 + c0 - (warp & 3) * 32;
                         bks[0] = at[31 - lane];
                         if (lane > 0) bks[1] = at[lane - 32];
@@ -376,7 +390,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     if (++st == ST) { st = 0; tp ^= 1; }
                     par ^= 1;
                     if (!HDT_AGREE()) break;
-                    if (!(sums && side == 0 && any)) continue;
+                    if (!(sums && near && any)) continue;
                     __syncwarp();
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
@@ -399,17 +413,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     float v0, v1;
                     unpack2(row_sum, v0, v1);
                     sSum[(2 * x + qh) * 128 + rl] = v0 + v1;
-                } else if (sums) {
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) far_sum[g] += __shfl_xor_sync(0xffffffffu, far_sum[g], o);
-                    __syncwarp();
-                    if (lane == 0) {
-                        sum[a.dist.bucket[a.dist.n - 1]] += far_sum[0];
-                        if (!a.causal) sum[a.dist.bucket[0]] += far_sum[1];
-                    }
-                }
+                } else if (sums) flush(far_sum, nt > near0 ? a.dist.n - 1 : 0);
                 mbar_arrive(sum_full);
                 ++uc;
             }
