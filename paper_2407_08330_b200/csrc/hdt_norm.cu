@@ -22,6 +22,9 @@ namespace hdt {
 namespace {
 
 constexpr int THREADS = 128;
+__host__ __device__ constexpr int cta_threads(int wpr) { return wpr > 1 ? 32 * wpr : THREADS; }      // WPR > 1: a row to a CTA
+// CTAs of the backward that are resident on an SM, by what a warp keeps of a row.
+__host__ __device__ constexpr int bwd_ctas(int wpr, int nv) { return wpr == 16 ? 1 : wpr == 2 ? 7 : nv == 1 ? 5 : 3; }
 
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
@@ -74,7 +77,7 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float2 (&s)[2][WPR]
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
-__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS) k_norm_fwd(const NormArgs a) {
+__global__ void __launch_bounds__(cta_threads(WPR)) k_norm_fwd(const NormArgs a) {
     __shared__ float s_sum[WPR];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LPR;
     const int first = WPR > 1 ? blockIdx.x : (blockIdx.x * (THREADS / 32) + warp) * (32 / LPR) + lane / LPR;
@@ -138,8 +141,8 @@ __global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS) k_norm_fwd(const
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
-__global__ void __launch_bounds__(WPR > 4 ? 32 * WPR : THREADS, WPR > 4 ? 1 : WPR == 4 && NV == 1 ? 5 : 3) k_norm_bwd(const NormArgs a) {
-    constexpr int NW = WPR > 4 ? WPR : THREADS / 32, RPC = WPR > 1 ? 1 : NW * (32 / LPR);   // rows of a CTA at a time
+__global__ void __launch_bounds__(cta_threads(WPR), bwd_ctas(WPR, NV)) k_norm_bwd(const NormArgs a) {
+    constexpr int NW = cta_threads(WPR) / 32, RPC = WPR > 1 ? 1 : NW * (32 / LPR);   // rows of a CTA at a time
     __shared__ float2 s_sum[2][WPR];
     __shared__ float s_col[WPR > 1 ? 1 : NW * 8 * 32];
     pdl_launch_dependents();
@@ -346,8 +349,8 @@ int norm_types(const NormArgs &a, int dtype, int w_dtype, bool vec, cudaStream_t
     return vec ? norm_pick<K, __nv_bfloat16, __nv_bfloat16, true>(a, st) : norm_pick<K, __nv_bfloat16, __nv_bfloat16, false>(a, st);
 }
 
-// The backward keeps two sums a column and the next row besides, so a warp holds a row of up to 768 (aligned bf16) or 512 columns,
-// four warps one of up to 2048, sixteen up to 8192 (1024 columns on one warp spilled 500 bytes a thread).
+// The backward keeps two sums a column and the next row besides, so a warp holds a row of up to 768 (aligned bf16) or 512 columns, two
+// (aligned bf16) or four warps one of up to 1024, four one of up to 2048, sixteen up to 8192 (1024 columns on one warp spilled 500 bytes a thread).
 template <template <typename, typename, bool, int, int, int> class K, typename T, typename W, bool VEC>
 int norm_pick_bwd(const NormArgs &a, cudaStream_t st) {
     const int c = a.cols;
@@ -358,6 +361,8 @@ int norm_pick_bwd(const NormArgs &a, cudaStream_t st) {
     if (c <= 512) return K<T, W, VEC, 32, 1, 2>::go(a, st);
     if constexpr (sizeof(T) == 2 && VEC)
         if (c <= 768) return K<T, W, VEC, 32, 1, 3>::go(a, st);
+    if constexpr (sizeof(T) == 2 && VEC)
+        if (c <= 1024) return K<T, W, VEC, 32, 2, 2>::go(a, st);
     if (c <= 1024) return K<T, W, VEC, 32, 4, 1>::go(a, st);
     if (c <= 2048) return K<T, W, VEC, 32, 4, 2>::go(a, st);
     if (c <= 4096) return K<T, W, VEC, 32, 16, 1>::go(a, st);
@@ -370,27 +375,27 @@ int norm_types_bwd(const NormArgs &a, int dtype, int w_dtype, bool vec, cudaStre
     return vec ? norm_pick_bwd<K, __nv_bfloat16, __nv_bfloat16, true>(a, st) : norm_pick_bwd<K, __nv_bfloat16, __nv_bfloat16, false>(a, st);
 }
 
-int rows_at_once(int cols) { return cols > 768 ? 1 : cols > 128 ? 4 : cols > 64 ? 8 : cols > 32 ? 16 : 32; }
-// CTAs of the backward, and so partial rows: those that are resident at once (any number is right).
-int bwd_grid(int64_t rows, int cols) {
-    const int64_t need = (rows + rows_at_once(cols) - 1) / rows_at_once(cols);
-    const int64_t most = (int64_t)PLAN_SMS * (cols > 2048 ? 1 : cols > 1024 ? 3 : cols > 768 ? 5 : 3);
-    return (int)(need < most ? need : most);
+// An upper limit of the backward's CTAs, and so of its partial rows.
+int64_t bwd_most(int64_t rows, int cols) {
+    const int at_once = cols > 512 ? 1 : cols > 128 ? 4 : cols > 64 ? 8 : cols > 32 ? 16 : 32;
+    const int64_t need = (rows + at_once - 1) / at_once, most = (int64_t)PLAN_SMS * bwd_ctas(2, 2);
+    return need < most ? need : most;
 }
 
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
 struct Fwd {
     static int go(const NormArgs &a, cudaStream_t st) {
         const int per = WPR > 1 ? 1 : THREADS / LPR;
-        HDT_CUDA_CHECK(launch_dependent(k_norm_fwd<T, W, VEC, LPR, WPR, NV>, false, dim3((a.rows + per - 1) / per), WPR > 4 ? 32 * WPR : THREADS, 0, st, a));
+        HDT_CUDA_CHECK(launch_dependent(k_norm_fwd<T, W, VEC, LPR, WPR, NV>, false, dim3((a.rows + per - 1) / per), cta_threads(WPR), 0, st, a));
         return HDT_OK;
     }
 };
 template <typename T, typename W, bool VEC, int LPR, int WPR, int NV>
-struct Bwd {
+struct Bwd {      // returns the number of CTAs (all resident at once), or an error
     static int go(const NormArgs &a, cudaStream_t st) {
-        HDT_CUDA_CHECK(launch_dependent(k_norm_bwd<T, W, VEC, LPR, WPR, NV>, false, dim3(bwd_grid(a.rows, a.cols)), WPR > 4 ? 32 * WPR : THREADS, 0, st, a));
-        return HDT_OK;
+        const int at_once = WPR > 1 ? 1 : THREADS / LPR, need = (a.rows + at_once - 1) / at_once, most = PLAN_SMS * bwd_ctas(WPR, NV), n = need < most ? need : most;
+        HDT_CUDA_CHECK(launch_dependent(k_norm_bwd<T, W, VEC, LPR, WPR, NV>, false, dim3(n), cta_threads(WPR), 0, st, a));
+        return n;
     }
 };
 
@@ -448,8 +453,8 @@ extern "C" int hdt_layer_norm_fwd(const void *x, const void *residual, const voi
 
 extern "C" size_t hdt_layer_norm_workspace_bytes(int64_t rows, int32_t cols) {
     if (rows < 0 || rows > 0x7fff0000LL || cols < 1 || cols > 8192) return 0;
-    const int g = bwd_grid(rows, cols);
-    return ((size_t)(g > 0 ? g : 1) * 2 * cols * 4 + 255) / 256 * 256;
+    const int64_t n = bwd_most(rows, cols);
+    return ((size_t)(n > 0 ? n : 1) * 2 * cols * 4 + 255) / 256 * 256;
 }
 
 extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const float *mean, const float *rstd, const void *weight, const int64_t *rng,
@@ -472,11 +477,13 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
     a.dx = p > 0.f ? d_x : nullptr;      // (a p that rounds to no dropout at all has its gradient too)
     a.part = (float *)workspace; a.rows = (int)rows; a.cols = cols;
     cudaStream_t st = (cudaStream_t)stream;
+    int n = 0;
     if (rows > 0) {
         const bool vec = cols % 8 == 0 && aligned16(d_y) && aligned16(d_h) && aligned16(h) && aligned16(weight) && aligned16(d_residual) && aligned16(d_x);
-        if (const int rc = norm_types_bwd<Bwd>(a, dtype, w_dtype, vec, st)) return rc;
+        n = norm_types_bwd<Bwd>(a, dtype, w_dtype, vec, st);
+        if (n < 0) return n;
     }
-    const int n = bwd_grid(rows, cols), ctas = (2 * cols + 31) / 32;
+    const int ctas = (2 * cols + 31) / 32;
     if (w_dtype == HDT_F32) HDT_CUDA_CHECK(launch_dependent(k_norm_columns<float>, rows > 0, dim3(ctas), 1024, 0, st, a.part, n, cols, (float *)d_weight, (float *)d_bias));
     else HDT_CUDA_CHECK(launch_dependent(k_norm_columns<__nv_bfloat16>, rows > 0, dim3(ctas), 1024, 0, st, a.part, n, cols, (__nv_bfloat16 *)d_weight, (__nv_bfloat16 *)d_bias));
     return HDT_OK;
