@@ -269,35 +269,35 @@ __global__ void __launch_bounds__(1024) k_norm_columns(const float *part, int n,
     }
 }
 
-template <typename T, bool VEC, int LPR>
+// Four pieces of a lane at a time: four chunks of a row, or, where a row is one chunk (ONE), four rows.
+template <typename T, bool VEC, int LPR, bool ONE>
 __global__ void __launch_bounds__(256, 4) k_dropout(const T *x, const T *residual, T *y, int rows, int cols, const Drop d) {
-    constexpr int U = 4;
+    constexpr int U = 4, RPW = 32 / LPR;
     const int lane = threadIdx.x & 31, l = lane % LPR;
-    const int first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / LPR) + lane / LPR;
-    const bool on = first < rows;
-    const int row = on ? first : rows - 1;
-    const size_t at = (size_t)row * cols;
-    const int chunks = (cols + 8 * LPR - 1) / (8 * LPR);
+    const int first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * RPW * (ONE ? U : 1) + lane / LPR;
+    const int chunks = ONE ? U : (cols + 8 * LPR - 1) / (8 * LPR);
     const PhiloxKey k = philox_key(d);
     for (int c0 = 0; c0 < chunks; c0 += U) {
         Raw8<T, VEC> rx[U], rr[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {      // (a chunk behind the row's end reads as zeros)
-            rx[i].template load<LPR>(x + at, c0 + i, l, cols);
-            if (residual != nullptr) rr[i].template load<LPR>(residual + at, c0 + i, l, cols);
+        for (int i = 0; i < U; ++i) {      // (a chunk behind the row's end reads as zeros, a row behind the last as the last)
+            const size_t at = (size_t)min(first + (ONE ? i * RPW : 0), rows - 1) * cols;
+            rx[i].template load<LPR>(x + at, ONE ? 0 : c0 + i, l, cols);
+            if (residual != nullptr) rr[i].template load<LPR>(residual + at, ONE ? 0 : c0 + i, l, cols);
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            if (c0 + i >= chunks) break;
+            if (!ONE && c0 + i >= chunks) break;
+            const int row = first + (ONE ? i * RPW : 0), c = ONE ? 0 : c0 + i;
             float v[8], r[8];
             rx[i].get(v);
-            drop8<LPR, VEC>(k, d, row, c0 + i, l, v);
+            drop8<LPR, VEC>(k, d, row, c, l, v);
             if (residual != nullptr) {
                 rr[i].get(r);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += r[e];
             }
-            if (on) store8<LPR, VEC>(y + at, c0 + i, l, cols, v);
+            if (row < rows) store8<LPR, VEC>(y + (size_t)row * cols, c, l, cols, v);
         }
     }
 }
@@ -401,15 +401,16 @@ struct Bwd {      // returns the number of CTAs (all resident at once), or an er
 
 template <typename T, bool VEC>
 int dropout_pick(const void *x, const void *res, void *y, int rows, int cols, const Drop &d, cudaStream_t st) {
-    auto go = [&](auto *kern, int lpr) -> int {
-        const int per = 8 * (32 / lpr);
+    auto go = [&](auto *kern, int rows_of_warp) -> int {
+        const int per = 8 * rows_of_warp;
         HDT_CUDA_CHECK(launch_dependent(kern, false, dim3((rows + per - 1) / per), 256, 0, st, (const T *)x, (const T *)res, (T *)y, rows, cols, d));
         return HDT_OK;
     };
-    if (cols <= 32) return go(k_dropout<T, VEC, 4>, 4);
-    if (cols <= 64) return go(k_dropout<T, VEC, 8>, 8);
-    if (cols <= 128) return go(k_dropout<T, VEC, 16>, 16);
-    return go(k_dropout<T, VEC, 32>, 32);
+    if (cols <= 32) return go(k_dropout<T, VEC, 4, true>, 32);
+    if (cols <= 64) return go(k_dropout<T, VEC, 8, true>, 16);
+    if (cols <= 128) return go(k_dropout<T, VEC, 16, true>, 8);
+    if (cols <= 256) return go(k_dropout<T, VEC, 32, true>, 4);
+    return go(k_dropout<T, VEC, 32, false>, 1);
 }
 
 }  // namespace
