@@ -435,7 +435,7 @@ def hdt_layer_norm_fwd(x, weight, bias, eps=1e-5, residual=None, p=0.0, rng=None
     if h is None and (residual is not None or p > 0):
         h = torch.empty_like(x)
     if mean is None:
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
     if rstd is None:
         rstd = torch.empty_like(mean)
     rc = (_lib or lib()).hdt_layer_norm_fwd(x.data_ptr(), _ptr(residual), weight.data_ptr(), bias.data_ptr(), _rng(rng, p), int(site), float(p), rows, cols, dt,
@@ -464,7 +464,7 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
     d_weight = torch.empty_like(weight) if d_weight is None else d_weight
     d_bias = torch.empty_like(weight) if d_bias is None else d_bias
     if workspace is None:
-        workspace = torch.empty(max(hdt_layer_norm_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=h.device)
+        workspace = h.new_empty(max(hdt_layer_norm_workspace_bytes(rows, cols), 256), dtype=torch.uint8)
     if mean.numel() != rows or rstd.numel() != rows or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
         raise HdtError(-1, "mean and rstd must be float32, one element per row")
     rc = (_lib or lib()).hdt_layer_norm_bwd(d_y.data_ptr(), _ptr(d_h), h.data_ptr(), mean.data_ptr(), rstd.data_ptr(), weight.data_ptr(), _rng(rng, p), int(site),
@@ -511,9 +511,9 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
     if lse is not None and (lse.shape != (H, Tq) or lse.dtype != torch.float32):
         raise HdtError(-1, "lse must be float32 [heads, rows of q]")
     out = torch.empty_like(q) if out is None else out
-    lse = torch.empty((H, Tq), dtype=torch.float32, device=q.device) if lse is None else lse
+    lse = q.new_empty((H, Tq), dtype=torch.float32) if lse is None else lse
     if workspace is None:
-        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, False)), dtype=torch.uint8, device=q.device)
+        workspace = q.new_empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, False)), dtype=torch.uint8)
     rc = (_lib or lib()).hdt_self_attn_fwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                            _ptr(bias), n, int(max_distance), int(bool(causal)), out.data_ptr(), lse.data_ptr(), H, d, _DTYPES[q.dtype],
                                            float(softmax_scale), workspace.data_ptr(), workspace.numel(), _stream())
@@ -539,7 +539,7 @@ def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=Non
     if bias is not None and d_bias is None:
         d_bias = torch.empty_like(bias)
     if workspace is None:
-        workspace = torch.empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, True)), dtype=torch.uint8, device=q.device)
+        workspace = q.new_empty(max(256, hdt_self_workspace_bytes(B, Tq, Tk, H, d, n, max_distance, bool(causal), q.dtype, True)), dtype=torch.uint8)
     rc = (_lib or lib()).hdt_self_attn_bwd(cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), _ptr(seqlens_k), B, Tq, Tk, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                            _ptr(bias), n, int(max_distance), int(bool(causal)), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(), dq.data_ptr(),
                                            dk.data_ptr(), dv.data_ptr(), _ptr(d_bias), H, d, _DTYPES[q.dtype], float(softmax_scale), workspace.data_ptr(),
