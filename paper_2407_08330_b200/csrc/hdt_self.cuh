@@ -65,6 +65,10 @@ __host__ __device__ __forceinline__ int self_first_row(int causal, int k, int nq
     return r < 0 ? 0 : r > nq ? nq : r;
 }
 
+// The k-th unit of CTA `cta` of `ctas`, from a list ordered by cost: there and back again, so that who begins with the dearest
+// goes on with the cheapest (1 x 4096 tokens, 12 heads: a CTA's most tiles 40 -> 32).  Grows with k.
+__device__ __forceinline__ int self_unit(int k, int cta, int ctas) { return k * ctas + (k & 1 ? ctas - 1 - cta : cta); }
+
 struct SelfFwdArgs {
     SelfLists q;             // blocks of block_rows rows
     int block_rows;

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
             const int w = warp >> 2, rl = tid & 127;
             const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16, tm_s = tmem + 128u * w + lane_base, tm_o = tmem + TM_O + D * w + lane_base;
             int ns = 0, near_no = 0, nu = 0;
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            for (int k = 0, u; ok && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const SelfBlk b = a.q.blk[u / H];
                 const int h = u % H, nt = key_tiles(b, w), row = b.r0 + 128 * w + rl;
                 const bool valid = 128 * w < a.block_rows && row < b.nq;
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
         } else if (warp == 8) {
             // ================= load warp =================
             int uq[2] = {0, 0}, kt = 0, nfix = 0;
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            for (int k = 0, u; ok && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const SelfBlk b = a.q.blk[u / H];
                 const int h = u % H, nt[2] = {key_tiles(b, 0), key_tiles(b, 1)}, n = max(nt[0], nt[1]);
                 auto load = [&](uint8_t *dst, const CUtensorMap *tm, int row, uint64_t *bar) {
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
             };
             uint32_t uq[2] = {0, 0}, np[2] = {0, 0}, st = 0, round = 0;      // ring stage of this tile and parity of its use
             bool go = true;
-            for (int u = blockIdx.x; u < n_units && go; u += gridDim.x) {
+            for (int k = 0, u; go && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const SelfBlk b = a.q.blk[u / H];
                 const int nt[2] = {__shfl_sync(0xffffffffu, key_tiles(b, 0), 0), __shfl_sync(0xffffffffu, key_tiles(b, 1), 0)}, n = max(nt[0], nt[1]);
                 if (n == 0) continue;

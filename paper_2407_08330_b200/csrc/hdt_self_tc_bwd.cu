@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                 if (lane == 0) sum[a.dist.bucket[at]] += v;
                 __syncwarp();
             };
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            for (int k = 0, u; ok && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 // (what a unit needs in its loop, and no more: p and d fill the registers)
                 int nt, first, end;            // tiles; columns that this lane's row pairs with, from c0 on
                 int whole0, whole1;            // tiles in which every lane of the warp keeps all its columns
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
         } else if (warp == W_LOAD) {
             // ================= load warp =================
             int t = 0, uc = 0, nfix = 0;
-            for (int u = blockIdx.x; u < n_units && ok; u += gridDim.x) {
+            for (int k = 0, u; ok && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const Unit x = unit(u);
                 if (x.nt == 0) continue;
                 const int rb = uc % RES, rround = uc / RES;
@@ -531,11 +531,14 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             };
             // Tile by tile: this one's products with P and dS, and between them S and dP of the tiles behind it.  What this warp
             // keeps is counted: every instruction of it is on the critical chain.
-            int u_next = blockIdx.x;
+            int k_next = 0;
             auto next_nt = [&]() {      // tiles of the next unit that has any, 0 behind the last
-                int n = 0;
-                for (; u_next < n_units && n == 0; u_next += gridDim.x) n = __shfl_sync(0xffffffffu, unit(u_next).nt, 0);
-                return n;
+                for (int u; (u = self_unit(k_next, blockIdx.x, gridDim.x)) < n_units;) {
+                    ++k_next;
+                    const int n = __shfl_sync(0xffffffffu, unit(u).nt, 0);
+                    if (n > 0) return n;
+                }
+                return 0;
             };
             auto wait = [&](uint64_t *bar, uint32_t parity, int site) {      // (the whole warp knows whether it ended well)
                 HDT_WAIT(bar, parity, site);
@@ -616,14 +619,15 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
         } else if (warp < W_LOAD) {
             // ================= drain group =================
             const int rl = tid & 127;
-            int uc = 0, um = 0, u_move = blockIdx.x;
+            int uc = 0, um = 0, k_move = 0;
             // the resident tiles of the next unit that has any: from shared memory into TMEM, once the last products with those
             // of two units before are through
             auto move_next = [&]() {
                 if (!RTM) return;
-                for (; u_move < n_units && unit(u_move).nt == 0; u_move += gridDim.x) {}
-                if (u_move >= n_units) return;
-                u_move += gridDim.x;
+                int u;
+                while ((u = self_unit(k_move, blockIdx.x, gridDim.x)) < n_units && unit(u).nt == 0) ++k_move;
+                if (u >= n_units) return;
+                ++k_move;
                 const uint8_t *r = sR + (um % RES) * 2 * TILE;
                 HDT_WAIT(&r_full[um % RES], (um / RES) & 1, 16);
                 if (um > 1) HDT_WAIT(&r_free[um & 1], ((um >> 1) - 1) & 1, 17);
@@ -647,7 +651,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             };
             move_next();
             move_next();
-            for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
+            for (int k = 0, u; (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const Unit U = unit(u);
                 const int nrows = min(128, (ROWS ? U.b.nq : U.b.nk) - U.b.r0);
                 float r = 0.f;
