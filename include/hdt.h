@@ -13,6 +13,9 @@
  *
  * The mask is the same for all heads and differs per sequence.
  *
+ * Beside it, for the blocks of an encoder-decoder model around that attention (further down): hdt_dropout,
+ * hdt_layer_norm_fwd / _bwd, hdt_self_attn_fwd / _bwd and the cross-attention hdt_cross_attn_fwd / _bwd.
+ *
  * Calling sequence:  hdt_build_index  (once per batch of documents; the index is valid for all
  * layers, heads, forward and backward)  ->  hdt_attn_fwd / hdt_attn_bwd  (any number of times)
  * ->  hdt_index_destroy.

@@ -21,6 +21,7 @@ struct PrepArgs {
     const int32_t *cu_q, *cu_k, *len_k;
     int B, Tq, Tk, H, n_lists;
     PrepList list[2];
+    int behind;               // launched as a programmatic dependent of a kernel of which it reads nothing: it ends behind it
     SelfRel rel;
     const void *table;
     int dtype;
@@ -80,10 +81,14 @@ __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ Prep
     pdl_launch_dependents();
     if ((int)blockIdx.x >= a.n_lists) {      // the bias by distance
         const int i = ((int)blockIdx.x - a.n_lists) * 1024 + t;
-        if (i >= a.n) return;
+        if (i >= a.n) {
+            if (a.behind) pdl_wait();
+            return;
+        }
         const int bk = self_bucket(a.rel, a.lo + i);
         a.bucket[i] = (unsigned char)bk;
         for (int h = 0; h < a.H; ++h) a.bias[(size_t)h * a.n + i] = bias_base2(a.table, (size_t)bk * a.H + h, a.dtype);
+        if (a.behind) pdl_wait();
         return;
     }
     const PrepList L = a.list[blockIdx.x];
@@ -134,6 +139,7 @@ __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ Prep
         L.out[atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1)] = x;
     }
     if (t == 0) *L.count = total;
+    if (a.behind) pdl_wait();
 }
 
 // Sums of the blocks' partial sums, a CTA per head; threads of one bucket take every G-th block, then meet in order.
@@ -519,7 +525,8 @@ int prepare(const Layout &L, char *ws, const int32_t *cu_q, const int32_t *cu_k,
     }
     out->q = SelfLists{p.list[0].out, count, L.most_q};
     out->k = SelfLists{p.list[1].out, count + 1, L.most_k};
-    HDT_CUDA_CHECK(launch_dependent(k_self_prep, false, dim3((unsigned)(p.n_lists + (p.n + 1023) / 1024)), 1024, 0, st, p));
+    p.behind = bwd && Tq > 0;      // (delta's kernel, which is not a dependent itself)
+    HDT_CUDA_CHECK(launch_dependent(k_self_prep, p.behind != 0, dim3((unsigned)(p.n_lists + (p.n + 1023) / 1024)), 1024, 0, st, p));
     return HDT_OK;
 }
 
@@ -607,13 +614,14 @@ extern "C" int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         for (const void *x : {q, k, v, o, d_o, (const void *)dq, (const void *)dk, (const void *)dv})
             if (const int rc = ptr_check(x, who)) return rc;
         if (!lse || ((uintptr_t)lse & 3)) return set_error(HDT_ERR_INVALID_ARG, "%s: null or misaligned tensor", who);
+        // (delta first: the preparation runs beside it)
+        if (const int rc = launch_delta(o, d_o, (float *)(ws + L.delta), total_q, heads, head_dim, dtype, st)) return rc;
         if (const int rc = prepare(L, ws, cu_seqlens_q, cu_seqlens_k, seqlens_k, batch, total_q, total_k, heads, num_buckets, max_distance, causal, bias, dtype, 1, st, &p)) return rc;
         const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
         SelfBwdArgs a{};
         a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0; a.buckets = num_buckets;
         a.qp = q; a.kp = k; a.vp = v; a.dop = d_o; a.lse = lse; a.delta = (float *)(ws + L.delta); a.dq = dq; a.dk = dk; a.dv = dv;
         a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.status = device_status_ptr();
-        if (const int rc = launch_delta(o, d_o, (float *)(ws + L.delta), total_q, heads, head_dim, dtype, st)) return rc;
         SelfBwdArgs keys = a, rows = a;
         keys.blk = p.k;
         rows.blk = p.q;
