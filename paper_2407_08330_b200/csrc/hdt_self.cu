@@ -168,6 +168,7 @@ struct StepArgs {
     void *o;
     float *lse, *part_o, *part_ml;      // [slot][H][D], [slot][H][2]; a slot per (item, row of its group)
     float scale_log2;
+    int *before;                        // [B]: items of the documents before (many documents), or nullptr: every warp counts them itself
     SelfRel rel;
 };
 template <int RG>
@@ -180,9 +181,53 @@ struct StepDoc {      // how a document's work is cut: row groups x pieces of ke
     }
     __device__ __forceinline__ int items() const { return groups * pieces; }
 };
-// The document that item x, or row x, lies in, and how many items come before the document (whole warp).
+// Items before every document.
+template <int RG>
+__global__ void __launch_bounds__(1024) k_self_items(const __grid_constant__ StepArgs a) {
+    __shared__ int s_warp[32], s_sum;
+    pdl_launch_dependents();
+    int base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 1024) {
+        const int b = b0 + (int)threadIdx.x;
+        int n = 0;
+        if (b < a.B) n = StepDoc<RG>(document(a.cu_q, a.cu_k, a.len_k, b, a.Tq, a.Tk), a.piece).items();
+        const int pre = scan1024(n, s_warp);
+        if (b < a.B) a.before[b] = base + pre - n;
+        if (threadIdx.x == 1023) s_sum = pre;
+        __syncthreads();
+        base += s_sum;
+        __syncthreads();
+    }
+}
+// The last of n ascending numbers that is at most x (-1: none), by a whole warp, thirty-two at a time.
+template <class F>
+__device__ __forceinline__ int last_at_most(int n, int x, F get) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, len = n;
+    while (len > 0) {
+        const int step = (len + 31) / 32, i = lo + lane * step;
+        const unsigned m = __ballot_sync(0xffffffffu, lane * step < len && get(i) <= x);
+        if (m == 0) return lo - 1;
+        const int k = 31 - __clz(m);
+        if (step == 1) return lo + k;
+        const int end = lo + len;
+        lo += k * step;
+        len = min(step, end - lo);
+    }
+    return -1;
+}
+// The document that item x, or row x, lies in, and how many items come before the document (whole warp).  Up to 64 documents, whose
+// loads are two rounds, every warp counts; beyond, k_self_items has, and the document is searched for (65 documents: 21.5 us counted, 22.3
+// searched; 128: 48.9 and 48.1; 1000: 268 and 82; 4000: 3138 and 220).
 template <int RG, bool BY_ROW>
 __device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &before) {
+    if (a.before != nullptr) {
+        const int b = BY_ROW ? last_at_most(a.B, x, [&](int i) { return a.cu_q[i]; }) : last_at_most(a.B, x, [&](int i) { return a.before[i]; });
+        if (b < 0) return false;
+        d = document(a.cu_q, a.cu_k, a.len_k, b, a.Tq, a.Tk);
+        before = a.before[b];
+        return BY_ROW ? x >= d.q0 && x < d.q0 + d.nq : (unsigned)x - (unsigned)before < (unsigned)StepDoc<RG>(d, a.piece).items();
+    }
     const int lane = threadIdx.x & 31;
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -224,6 +269,7 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
     const float far_bias = a.rel.on ? bias_base2(a.table, (size_t)self_bucket(a.rel, a.rel.far) * a.H + h, a.dtype) : 0.f;
     Doc d;
     int before;
+    pdl_wait();
     if (item >= a.items || !find_doc<RG, false>(a, item, d, before)) return;
     const StepDoc<RG> cut(d, a.piece);
     const int g = (item - before) / cut.pieces, pc = (item - before) % cut.pieces, r0 = g * RG, nr = min(RG, d.nq - r0);
@@ -310,13 +356,14 @@ __global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepA
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x / a.H, h = blockIdx.x % a.H;
     Doc d;
     int before;
-    // (before the wait: the kernel in front does not write the offsets, and began behind what did)
+    // (before the wait where every warp counts: the kernel in front does not write the offsets, and began behind what did)
+    if (a.before != nullptr) pdl_wait();
     const bool found = find_doc<RG, true>(a, row, d, before);
     pdl_wait();
     if (!found) return;
     const StepDoc<RG> cut(d, a.piece);
     const int r = row - d.q0, first = before + (r / RG) * cut.pieces;
-    if (cut.pieces == 1 || first + cut.pieces > a.items) return;      // written by the one warp that had the row (or no valid offsets)
+    if (cut.pieces == 1 || first < 0 || cut.pieces > a.items - first) return;      // written by the one warp that had the row (or no valid offsets)
     auto at = [&](int i) { return ((size_t)(first + i) * RG + r % RG) * a.H + h; };
     float m = -INFINITY, l = 0.f, acc[E];
 #pragma unroll
@@ -413,6 +460,7 @@ void rel_fill(SelfRel *r, int buckets, int max_distance, int causal) {
 }
 
 size_t al(size_t n) { return (n + 255) / 256 * 256; }
+constexpr int STEP_COUNTED = 64;  // documents up to which every warp of a step counts their items itself
 constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which a call is a step of decoding
 bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
 // Keys of a piece: fourteen warps to an SM if the rows are one per document (sixteen fit at once, and documents round up), at least 64.
@@ -426,7 +474,7 @@ int step_group(int B, int Tq) { return Tq <= B ? 1 : STEP_ROWS; }
 
 struct Layout {
     int rows_q, most_q, most_k, n;
-    size_t count, raw, q, k, bias, bucket, delta, part, part_o, part_ml, total;
+    size_t count, raw, q, k, bias, bucket, delta, part, part_o, part_ml, before, total;
 };
 long long blocks(int T, int B, int rows) { return (long long)T / rows + B; }
 Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance, int causal, int dtype, int bwd) {
@@ -438,6 +486,7 @@ Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance
         const long long slots = step_items(B, Tq, Tk, H, rg) * rg;
         L.part_o = take((size_t)slots * H * D * 4);
         L.part_ml = take((size_t)slots * H * 8);
+        if (B > STEP_COUNTED) L.before = take((size_t)B * 4);
     } else {
         L.rows_q = dtype == HDT_F32 ? SELF_F32_ROWS : 128;
         // two row tiles to a unit (they share the K and V tiles) where that leaves a unit for every SM
@@ -491,7 +540,8 @@ int ws_check(const void *ws, size_t n, size_t need, const char *who) {
 template <int D, bool BF16, int RG>
 int step_go(StepArgs a, cudaStream_t st) {
     a.items = (int)step_items(a.B, a.Tq, a.Tk, a.H, RG);
-    HDT_CUDA_CHECK(launch_dependent(k_self_step<D, BF16, RG>, false, dim3((unsigned)(((long long)a.items * a.H + 3) / 4)), 128, 0, st, a));
+    if (a.before != nullptr) HDT_CUDA_CHECK(launch_dependent(k_self_items<RG>, false, dim3(1), 1024, 0, st, a));
+    HDT_CUDA_CHECK(launch_dependent(k_self_step<D, BF16, RG>, a.before != nullptr, dim3((unsigned)(((long long)a.items * a.H + 3) / 4)), 128, 0, st, a));
     if (a.Tk <= a.piece) return HDT_OK;      // no document of several pieces
     HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)a.Tq * (unsigned)a.H), 128, 0, st, a));
     return HDT_OK;
@@ -576,6 +626,7 @@ extern "C" int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         s.piece = step_piece(total_k, heads); s.dtype = dtype;
         s.q = q; s.k = k; s.v = v; s.table = bias; s.o = o; s.lse = lse; s.part_o = (float *)(ws + L.part_o); s.part_ml = (float *)(ws + L.part_ml);
         s.scale_log2 = scale * LOG2E;
+        s.before = batch > STEP_COUNTED ? (int *)(ws + L.before) : nullptr;
         s.rel.causal = causal;
         if (num_buckets > 0) rel_fill(&s.rel, num_buckets, max_distance, causal);
         if (head_dim == 64) return dtype == HDT_BF16 ? step_rows<64, true>(s, st) : step_rows<64, false>(s, st);

@@ -155,7 +155,8 @@ def test_unused_rows_of_a_cache_and_behind_the_last_document(dtype, causal):
 @pytest.mark.parametrize("d, H", [(64, 12), (128, 5), (64, 1)])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("lens", [([1], [1]), ([1] * 6, [1, 2000, 64, 65, 700, 0]), ([4, 1, 2, 7, 0], [30, 500, 100, 90, 5]), ([8, 0, 0], [900, 4, 0]),
-                                  ([1] * 40, list(range(40))), ([2] * 3, [1, 1, 129]), ([0, 0, 3], [5, 0, 2])], ids=lambda x: "x".join(map(str, x[0][:5])))
+                                  ([1] * 40, list(range(40))), ([2] * 3, [1, 1, 129]), ([0, 0, 3], [5, 0, 2]),
+                                  ([1, 0, 3, 0, 0, 1, 7] * 12, [9, 4, 300, 0, 8, 0, 70] * 12), ([1] * 1100, [i % 9 for i in range(1099)] + [900])], ids=lambda x: "x".join(map(str, x[0][:5])))
 def test_decoding(dtype, d, H, causal, lens):
     for room in (0, 5):
         c = Case(*lens, H, d, dtype, causal, room=room, behind=3)
