@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(384, 1) k_self_fwd(const __grid_constant__ CUt
                             tmem_st32(tm_o + 32u * i, o);
                         }
                     }
-                    const float cm = m == -INFINITY ? 0.f : c - m;      // (no key so far: exp2(-inf) = 0)
+                    const float cm = m == -INFINITY ? c : c - m;      // (no key so far: all of s, or c, is -inf, and exp2(-inf) = 0)
                     f2 sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {

@@ -188,6 +188,21 @@ def test_shut_buckets(dtype, rows):
     assert all(torch.equal(got[n], want[n]) for n in got)
 
 
+@pytest.mark.parametrize("dtype, d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("rows", [[700, 400], [1, 1]])
+def test_shut_far_bucket(dtype, d, causal, rows):
+    """Nothing but the last bucket shut (whole tiles of it come first), or all but the first, or everything: logits that large that a
+    weight of a shut key would not stay finite."""
+    c = Case(rows, [700, 400], 3, d, dtype, causal, scale=20 / d ** 0.5)
+    c.bias[:, 0] = -torch.inf
+    c.bias[1 if causal else 31, 1] = -torch.inf
+    c.bias[15:16, 1] = -torch.inf
+    c.bias[31:, 1] = -torch.inf
+    c.bias[1:, 2] = -torch.inf
+    c.check(c.run(backward=rows[0] > 1))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_other_documents_stay_out_of_non_finite_ones(dtype, d):
