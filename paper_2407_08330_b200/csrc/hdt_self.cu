@@ -514,8 +514,8 @@ int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distan
     if (B < 0 || Tq < 0 || Tk < 0 || H < 1 || buckets < 0) return set_error(HDT_ERR_INVALID_ARG, "%s: negative size or no head", who);
     if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
-    if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7fffff00LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
-    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7fffff00LL || step_items(B, Tq, Tk, H, 1) * H > 0x7fffff00LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fffff00LL))
+    if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7ffff000LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
+    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, 1) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7ffff000LL))
         return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
     if (buckets > 0) {
         const int one = causal ? buckets : buckets / 2;
