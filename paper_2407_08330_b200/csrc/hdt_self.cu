@@ -168,7 +168,8 @@ struct StepArgs {
     void *o;
     float *lse, *part_o, *part_ml;      // [slot][H][D], [slot][H][2]; a slot per (item, row of its group)
     float scale_log2;
-    int *before;                        // [B]: items of the documents before (many documents), or nullptr: every warp counts them itself
+    int *before;                        // [B]: items of the documents before (many documents), and [B] whether any has several pieces; or
+                                        // nullptr: every warp counts them itself
     SelfRel rel;
 };
 template <int RG>
@@ -181,16 +182,20 @@ struct StepDoc {      // how a document's work is cut: row groups x pieces of ke
     }
     __device__ __forceinline__ int items() const { return groups * pieces; }
 };
-// Items before every document.
+// Items before every document, and whether there is anything to join.
 template <int RG>
 __global__ void __launch_bounds__(1024) k_self_items(const __grid_constant__ StepArgs a) {
     __shared__ int s_warp[32], s_sum;
     pdl_launch_dependents();
-    int base = 0;
+    int base = 0, several = 0;
     for (int b0 = 0; b0 < a.B; b0 += 1024) {
         const int b = b0 + (int)threadIdx.x;
         int n = 0;
-        if (b < a.B) n = StepDoc<RG>(document(a.cu_q, a.cu_k, a.len_k, b, a.Tq, a.Tk), a.piece).items();
+        if (b < a.B) {
+            const StepDoc<RG> cut(document(a.cu_q, a.cu_k, a.len_k, b, a.Tq, a.Tk), a.piece);
+            n = cut.items();
+            several |= cut.pieces > 1;
+        }
         const int pre = scan1024(n, s_warp);
         if (b < a.B) a.before[b] = base + pre - n;
         if (threadIdx.x == 1023) s_sum = pre;
@@ -198,6 +203,8 @@ __global__ void __launch_bounds__(1024) k_self_items(const __grid_constant__ Ste
         base += s_sum;
         __syncthreads();
     }
+    several = __syncthreads_or(several);
+    if (threadIdx.x == 0) a.before[a.B] = several;
 }
 // The last of n ascending numbers that is at most x (-1: none), by a whole warp, thirty-two at a time.
 template <class F>
@@ -357,7 +364,10 @@ __global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepA
     Doc d;
     int before;
     // (before the wait where every warp counts: the kernel in front does not write the offsets, and began behind what did)
-    if (a.before != nullptr) pdl_wait();
+    if (a.before != nullptr) {
+        pdl_wait();
+        if (a.before[a.B] == 0) return;
+    }
     const bool found = find_doc<RG, true>(a, row, d, before);
     pdl_wait();
     if (!found) return;
@@ -486,7 +496,7 @@ Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance
         const long long slots = step_items(B, Tq, Tk, H, rg) * rg;
         L.part_o = take((size_t)slots * H * D * 4);
         L.part_ml = take((size_t)slots * H * 8);
-        if (B > STEP_COUNTED) L.before = take((size_t)B * 4);
+        if (B > STEP_COUNTED) L.before = take((size_t)(B + 1) * 4);
     } else {
         L.rows_q = dtype == HDT_F32 ? SELF_F32_ROWS : 128;
         // two row tiles to a unit (they share the K and V tiles) where that leaves a unit for every SM
