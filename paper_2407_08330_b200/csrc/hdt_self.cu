@@ -355,19 +355,14 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
     }
 }
 
-// The pieces of a row, a CTA per (row, head): its four warps take every fourth piece, four of them in flight, and meet in order.
+// The pieces of a row, a CTA: its four warps take every fourth piece, four of them in flight, and meet in order.
 template <int D, bool BF16, int RG>
-__global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepArgs a) {
+__device__ __forceinline__ void join_row(const StepArgs &a, int row, int h, float (*s_acc)[D], float (*s_ml)[2]) {
     constexpr int E = D / 32;
-    __shared__ float s_acc[4][D], s_ml[4][2];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x / a.H, h = blockIdx.x % a.H;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     Doc d;
     int before;
     // (before the wait where every warp counts: the kernel in front does not write the offsets, and began behind what did)
-    if (a.before != nullptr) {
-        pdl_wait();
-        if (a.before[a.B] == 0) return;
-    }
     const bool found = find_doc<RG, true>(a, row, d, before);
     pdl_wait();
     if (!found) return;
@@ -429,6 +424,19 @@ __global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepA
     else ((float *)a.o)[out] = y;
     if (threadIdx.x == 0) a.lse[(size_t)h * a.Tq + row] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
 }
+template <int D, bool BF16, int RG>
+__global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepArgs a) {
+    __shared__ float s_acc[4][D], s_ml[4][2];
+    if (a.before != nullptr) {
+        pdl_wait();
+        if (a.before[a.B] == 0) return;
+    }
+    const int n = a.Tq * a.H;
+    for (int x = blockIdx.x; x < n; x += gridDim.x) {      // (the host sees to it that this ends inside 32 bits)
+        if (x != (int)blockIdx.x) __syncthreads();
+        join_row<D, BF16, RG>(a, x / a.H, x % a.H, s_acc, s_ml);
+    }
+}
 
 // ---- host ---------------------------------------------------------------------------------------
 // Whether the distance d has passed the border far^(k/m) e^(1 - k/m), i.e. d^m e^k >= far^k e^m.  The difference of
@@ -471,6 +479,7 @@ void rel_fill(SelfRel *r, int buckets, int max_distance, int causal) {
 
 size_t al(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int STEP_COUNTED = 64;  // documents up to which every warp of a step counts their items itself
+constexpr int JOIN_CTAS = 16;      // CTAs of a join to an SM (all at once; more rows: one after the other)
 constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which a call is a step of decoding
 bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
 // Keys of a piece: fourteen warps to an SM if the rows are one per document (sixteen fit at once, and documents round up), at least 64.
@@ -525,7 +534,7 @@ int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distan
     if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7ffff000LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
-    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, 1) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7ffff000LL))
+    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, 1) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fff0000LL))
         return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
     if (buckets > 0) {
         const int one = causal ? buckets : buckets / 2;
@@ -553,7 +562,8 @@ int step_go(StepArgs a, cudaStream_t st) {
     if (a.before != nullptr) HDT_CUDA_CHECK(launch_dependent(k_self_items<RG>, false, dim3(1), 1024, 0, st, a));
     HDT_CUDA_CHECK(launch_dependent(k_self_step<D, BF16, RG>, a.before != nullptr, dim3((unsigned)(((long long)a.items * a.H + 3) / 4)), 128, 0, st, a));
     if (a.Tk <= a.piece) return HDT_OK;      // no document of several pieces
-    HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)a.Tq * (unsigned)a.H), 128, 0, st, a));
+    const long long rows = (long long)a.Tq * a.H, most = JOIN_CTAS * PLAN_SMS;
+    HDT_CUDA_CHECK(launch_dependent(k_self_join<D, BF16, RG>, true, dim3((unsigned)(rows < most ? rows : most)), 128, 0, st, a));
     return HDT_OK;
 }
 template <int D, bool BF16>
