@@ -7,7 +7,7 @@
 //
 // Decoding (few rows per document): bound by HBM, the keys and values once.  A warp takes a piece of a document's keys for
 // one head and up to four rows; every lane group has a softmax of its own, joined at the piece's end, the pieces by
-// k_self_join (8 documents of 4096 keys, 12 x 64 bf16: 21 us with both launches, 4.8 TB/s; four rows each 51).  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
+// k_self_join (8 documents of 4096 keys, 12 x 64 bf16: 19 us with both launches, 5.3 TB/s; four rows each 43).  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
 #include <math.h>
 
 #include "hdt_rows.cuh"
@@ -168,8 +168,8 @@ struct StepArgs {
     void *o;
     float *lse, *part_o, *part_ml;      // [slot][H][D], [slot][H][2]; a slot per (item, row of its group)
     float scale_log2;
-    int *before;                        // [B]: items of the documents before (many documents), and [B] whether any has several pieces; or
-                                        // nullptr: every warp counts them itself
+    int *before;                        // [B]: items of the documents before (many documents), [B] of all, and [B + 1] whether any has several
+                                        // pieces; or nullptr: every warp counts them itself
     SelfRel rel;
 };
 template <int RG>
@@ -204,7 +204,10 @@ __global__ void __launch_bounds__(1024) k_self_items(const __grid_constant__ Ste
         __syncthreads();
     }
     several = __syncthreads_or(several);
-    if (threadIdx.x == 0) a.before[a.B] = several;
+    if (threadIdx.x == 0) {
+        a.before[a.B] = base;
+        a.before[a.B + 1] = several;
+    }
 }
 // The last of n ascending numbers that is at most x (-1: none), by a whole warp, thirty-two at a time.
 template <class F>
@@ -224,8 +227,8 @@ __device__ __forceinline__ int last_at_most(int n, int x, F get) {
     return -1;
 }
 // The document that item x, or row x, lies in, and how many items come before the document (whole warp).  Up to 64 documents, whose
-// loads are two rounds, every warp counts; beyond, k_self_items has, and the document is searched for (65 documents: 21.5 us counted, 22.3
-// searched; 128: 48.9 and 48.1; 1000: 268 and 82; 4000: 3138 and 220).
+// loads are two rounds, every warp counts; beyond, k_self_items has, and the document is searched for (65 documents: 21.5 us
+// counted, 22.3 searched; 128: 48.9 and 48.1; 1000: 268 and 82; 4000: 3138 and 220; pieces since then other ones).
 template <int RG, bool BY_ROW>
 __device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &before) {
     if (a.before != nullptr) {
@@ -277,7 +280,7 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
     Doc d;
     int before;
     pdl_wait();
-    if (item >= a.items || !find_doc<RG, false>(a, item, d, before)) return;
+    if (item >= (a.before != nullptr ? min(a.items, a.before[a.B]) : a.items) || !find_doc<RG, false>(a, item, d, before)) return;
     const StepDoc<RG> cut(d, a.piece);
     const int g = (item - before) / cut.pieces, pc = (item - before) % cut.pieces, r0 = g * RG, nr = min(RG, d.nq - r0);
     const int pos0 = d.nk - d.nq + r0;                                  // position of the group's first row
@@ -429,7 +432,7 @@ __global__ void __launch_bounds__(128) k_self_join(const __grid_constant__ StepA
     __shared__ float s_acc[4][D], s_ml[4][2];
     if (a.before != nullptr) {
         pdl_wait();
-        if (a.before[a.B] == 0) return;
+        if (a.before[a.B + 1] == 0) return;
     }
     const int n = a.Tq * a.H;
     for (int x = blockIdx.x; x < n; x += gridDim.x) {      // (the host sees to it that this ends inside 32 bits)
@@ -482,13 +485,25 @@ constexpr int STEP_COUNTED = 64;  // documents up to which every warp of a step 
 constexpr int JOIN_CTAS = 16;      // CTAs of a join to an SM (all at once; more rows: one after the other)
 constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which a call is a step of decoding
 bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
-// Keys of a piece: fourteen warps to an SM if the rows are one per document (sixteen fit at once, and documents round up), at least 64.
-int step_piece(int Tk, int H) {
-    const long long per = ((long long)Tk * H + 14 * PLAN_SMS - 1) / (14 * PLAN_SMS);
-    return (int)((per < 64 ? 64 : per) + 15) / 16 * 16;
+// Keys of a piece, for documents of one length (the host knows no other): a piece is a warp, `most` of them are resident at once and
+// take turns in waves, and a warp takes about as long to begin as for 32 keys.  Of the pieces that fill 1 .. 8 waves, those that
+// are done first.  (Against one wave of fourteen warps to an SM: 8 x 4096 keys 19.4 -> 18.0 us, 128 x 500 48 -> 42, 100 x 3000 209 -> 155;
+// at most 256 keys: 100 x 3000 157, but 64 x 2000 72 -> 66 here, 128 x 500 50.)
+int step_piece(int B, int Tk, int H, int rg) {
+    const long long most = (rg == 1 ? 16 : 12) * PLAN_SMS, b = B > 0 ? B : 1, keys = (Tk + b - 1) / b;
+    long long best = 0, piece = 64;
+    for (int w = 1; w <= 8; ++w) {
+        const long long p = most * w / (b * H), most_p = (keys + 63) / 64, n = p < 1 ? 1 : p > most_p && most_p > 0 ? most_p : p;
+        const long long per = ((keys + n - 1) / n + 15) / 16 * 16, waves = (b * H * ((keys + per - 1) / (per > 0 ? per : 1)) + most - 1) / most, cost = waves * (per + 32);
+        if (w == 1 || cost < best) {
+            best = cost;
+            piece = per;
+        }
+    }
+    return (int)(piece < 64 ? 64 : piece);
 }
 // (a document of g row groups has at most keys / piece + g items)
-long long step_items(int B, int Tq, int Tk, int H, int rg) { return (long long)Tk / step_piece(Tk, H) + Tq / rg + B + 2; }
+long long step_items(int B, int Tq, int Tk, int H, int rg) { return (long long)Tk / step_piece(B, Tk, H, rg) + Tq / rg + B + 2; }
 int step_group(int B, int Tq) { return Tq <= B ? 1 : STEP_ROWS; }
 
 struct Layout {
@@ -505,7 +520,7 @@ Layout layout(int B, int Tq, int Tk, int H, int D, int buckets, int max_distance
         const long long slots = step_items(B, Tq, Tk, H, rg) * rg;
         L.part_o = take((size_t)slots * H * D * 4);
         L.part_ml = take((size_t)slots * H * 8);
-        if (B > STEP_COUNTED) L.before = take((size_t)(B + 1) * 4);
+        if (B > STEP_COUNTED) L.before = take(((size_t)B + 2) * 4);
     } else {
         L.rows_q = dtype == HDT_F32 ? SELF_F32_ROWS : 128;
         // two row tiles to a unit (they share the K and V tiles) where that leaves a unit for every SM
@@ -534,7 +549,7 @@ int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distan
     if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7ffff000LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
-    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, 1) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fff0000LL))
+    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, step_group(B, Tq)) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fff0000LL))
         return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
     if (buckets > 0) {
         const int one = causal ? buckets : buckets / 2;
@@ -643,7 +658,7 @@ extern "C" int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_
     if (is_step(batch, total_q)) {
         StepArgs s{};
         s.cu_q = cu_seqlens_q; s.cu_k = cu_seqlens_k; s.len_k = seqlens_k; s.B = batch; s.Tq = total_q; s.Tk = total_k; s.H = heads;
-        s.piece = step_piece(total_k, heads); s.dtype = dtype;
+        s.piece = step_piece(batch, total_k, heads, step_group(batch, total_q)); s.dtype = dtype;
         s.q = q; s.k = k; s.v = v; s.table = bias; s.o = o; s.lse = lse; s.part_o = (float *)(ws + L.part_o); s.part_ml = (float *)(ws + L.part_ml);
         s.scale_log2 = scale * LOG2E;
         s.before = batch > STEP_COUNTED ? (int *)(ws + L.before) : nullptr;
