@@ -339,7 +339,8 @@ int hdt_dropout(const void *x, const void *residual, const int64_t *rng, int32_t
  *   residual           NULL: none.  d_h, the gradient that h gets from the residual stream, NULL: none
  *   rng, site, p       as in hdt_dropout; p = 0: no dropout, rng may be NULL
  *   h                  may be x or residual; may be NULL where it is x itself (no residual and p = 0)
- *   d_x                written with p > 0 only (else it is d_residual); may be d_h, as may d_residual
+ *   d_x                with p > 0 a tensor of its own; with p = 0 it is d_residual: may be NULL or d_residual, any other one gets
+ *                      the same values.  May be d_h, as may d_residual
  *   workspace          device, >= hdt_layer_norm_workspace_bytes(rows, cols), 256-byte aligned: column sums of the
  *                      kernel's blocks, added up in a fixed order (the same bits every run)
  * Sizes and alignment as for hdt_dropout.  Without rows the backward writes zeros to d_weight and d_bias.

@@ -453,7 +453,7 @@ def hdt_layer_norm_workspace_bytes(rows, cols) -> int:
 def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, site=0, d_residual=None, d_x=None, d_weight=None, d_bias=None,
                        workspace=None):
     """Gradients (d_x, d_residual, d_weight, d_bias) of hdt_layer_norm_fwd; d_h is the gradient that h gets from elsewhere.
-    Without dropout d_x and d_residual are one tensor."""
+    Without dropout d_x and d_residual are one tensor, or, where d_x is given, two with the same values."""
     rows, cols, dt = _rows(h)
     _here(d_y, d_h, h, d_residual, d_x, mean, rstd, weight, d_weight, d_bias, workspace)
     _like(h, d_y, d_h, d_residual, d_x)

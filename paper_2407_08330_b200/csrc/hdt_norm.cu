@@ -470,6 +470,7 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
     if (!d_weight || !d_bias) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: null tensor pointer");
     if (rows > 0 && (!d_y || !h || !mean || !rstd || !weight || !d_residual || (p > 0.f && !d_x)))
         return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: null tensor pointer");
+    if (rows > 0 && p > 0.f && d_x == d_residual) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: with dropout d_x and d_residual are two tensors");
     const size_t need = hdt_layer_norm_workspace_bytes(rows, cols);
     if (!workspace || workspace_bytes < need) return set_error(HDT_ERR_WORKSPACE, "hdt_layer_norm_bwd: workspace %zu < required %zu", workspace_bytes, need);
     if ((uintptr_t)workspace & 255) return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: workspace must be 256-byte aligned");
@@ -478,7 +479,7 @@ extern "C" int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *
         (((uintptr_t)mean | (uintptr_t)rstd) & 3))
         return set_error(HDT_ERR_INVALID_ARG, "hdt_layer_norm_bwd: misaligned tensor");
     a.dy = d_y; a.dh = d_h; a.hin = h; a.mean_in = mean; a.rstd_in = rstd; a.weight = weight; a.dres = d_residual;
-    a.dx = p > 0.f ? d_x : nullptr;      // (a p that rounds to no dropout at all has its gradient too)
+    a.dx = d_x != d_residual ? d_x : nullptr;      // (a buffer of the caller's is written with and without dropout)
     a.part = (float *)workspace; a.rows = (int)rows; a.cols = cols;
     cudaStream_t st = (cudaStream_t)stream;
     int n = 0;
