@@ -65,23 +65,40 @@ __device__ __forceinline__ void dots(const float *a, const float *b, int ty, int
             s[i][j] = u + v;
         }
 }
+// One column of the sums below; ONLY: for the rows of `rows` (bit i: row 4 ty + i).
+template <int D, bool ONLY>
+__device__ __forceinline__ void accumulate_column(const float *p, const float *v, int c, int ty, int tx, f2 (&acc)[4][D / 32], unsigned rows) {
+    const float4 x = *reinterpret_cast<const float4 *>(p + c * PS + 4 * ty);
+    const f2 xs[4] = {pack2(x.x, x.x), pack2(x.y, x.y), pack2(x.z, x.z), pack2(x.w, x.w)};
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+        const float4 y = *reinterpret_cast<const float4 *>(v + c * Shape<D>::XS + 4 * tx + 64 * j);
+        const f2 y0 = pack2(y.x, y.y), y1 = pack2(y.z, y.w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (!ONLY || (rows >> i & 1u)) {
+                acc[i][2 * j] = fma2(xs[i], y0, acc[i][2 * j]);
+                acc[i][2 * j + 1] = fma2(xs[i], y1, acc[i][2 * j + 1]);
+            }
+    }
+}
 // acc[i][..] += sum over columns c of p[c][4 ty + i] v[c][4 tx + 64 j ..]
 template <int D>
 __device__ __forceinline__ void accumulate(const float *p, const float *v, int ty, int tx, f2 (&acc)[4][D / 32]) {
 #pragma unroll 4
-    for (int c = 0; c < R; ++c) {
-        const float4 x = *reinterpret_cast<const float4 *>(p + c * PS + 4 * ty);
-        const f2 xs[4] = {pack2(x.x, x.x), pack2(x.y, x.y), pack2(x.z, x.z), pack2(x.w, x.w)};
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            const float4 y = *reinterpret_cast<const float4 *>(v + c * Shape<D>::XS + 4 * tx + 64 * j);
-            const f2 y0 = pack2(y.x, y.y), y1 = pack2(y.z, y.w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[i][2 * j] = fma2(xs[i], y0, acc[i][2 * j]);
-                acc[i][2 * j + 1] = fma2(xs[i], y1, acc[i][2 * j + 1]);
-            }
-        }
+    for (int c = 0; c < R; ++c) accumulate_column<D, false>(p, v, c, ty, tx, acc, 15u);
+}
+// The same in a tile that causality cuts: row r has the columns c with c - r < edge (BELOW) or >= edge, and only those are added.  p of the
+// others is 0, but 0 times what is not finite is no number, and their rows must not reach this one.  (The four rows of a thread
+// differ in three columns; it skips what none of them has.)
+template <int D, bool BELOW>
+__device__ __forceinline__ void accumulate_cut(const float *p, const float *v, int ty, int tx, f2 (&acc)[4][D / 32], int edge) {
+    const int e = edge + 4 * ty, mid0 = min(max(e, 0), R), mid1 = min(max(e + 3, 0), R);      // between them not all four
+#pragma unroll 4
+    for (int c = BELOW ? 0 : mid1; c < (BELOW ? mid0 : R); ++c) accumulate_column<D, false>(p, v, c, ty, tx, acc, 15u);
+    for (int c = mid0; c < mid1; ++c) {
+        const unsigned above = 15u << (c - e + 1) & 15u;      // rows i with c < e + i (c - e is 0, 1 or 2)
+        accumulate_column<D, true>(p, v, c, ty, tx, acc, BELOW ? above : ~above);
     }
 }
 template <int N>
@@ -178,7 +195,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) k_self_fwd_f32(const Sel
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 4; ++i) scale_by(acc[i], sF[4 * ty + i]);
-            accumulate<D>(sP, sV, ty, tx, acc);
+            const int edge = b.off + b.r0 - k + 1;      // (causal: row r sees the columns below edge + r)
+            if (!a.causal || edge >= R) accumulate<D>(sP, sV, ty, tx, acc);
+            else accumulate_cut<D, true>(sP, sV, ty, tx, acc, edge);
         }
         __syncthreads();
 #pragma unroll
@@ -269,8 +288,13 @@ __device__ __forceinline__ void bwd_unit(const SelfBwdArgs &a, int u, float *sm)
                 sD[k * PS + r] = ds;
             }
         __syncthreads();
-        accumulate<D>(sD, sX, ty, tx, acc1);
-        if constexpr (!ROWS) accumulate<D>(sP, sY, ty, tx, acc2);
+        if (!a.causal || base >= R - 1) {      // all pairs of the tile
+            accumulate<D>(sD, sX, ty, tx, acc1);
+            if constexpr (!ROWS) accumulate<D>(sP, sY, ty, tx, acc2);
+        } else {      // rows: row r sees column c for base + r - c >= 0; keys: column c sees row r for base + c - r >= 0
+            accumulate_cut<D, ROWS>(sD, sX, ty, tx, acc1, ROWS ? base + 1 : -base);
+            if constexpr (!ROWS) accumulate_cut<D, ROWS>(sP, sY, ty, tx, acc2, -base);
+        }
         if (ROWS && a.part != nullptr && side == 0) {
             if (t < 2 * R - 1) {      // the diagonal row - column = t - 63
                 float v = 0.f;
