@@ -378,7 +378,8 @@ int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const fl
  * 2 <= n, num_buckets <= 128 and even if not causal, n / 2 < max_distance <= 32768.  head_dim 64 or 128; softmax_scale <= 0
  * means 1/sqrt(head_dim).  Rows that belong to no document, and k and v's beyond n_k, are left as they were in o, lse and
  * the gradients.  Offsets outside [0, total] are clamped; documents that overlap are not written whole.  bf16: a row of a document
- * that is not finite reaches the document's other rows of its tile; other documents never do.
+ * that is not finite reaches the document's other rows of its tile; fp32, and a step of decoding (below): the rows that
+ * see it, and no other.  Other documents never do.
  * Backward: dS = P o (d_o V^T - delta), dQ = scale dS K, dK = scale dS^T Q, dV = P^T d_o, d_bias[u][h] = sum of dS over the
  * pairs of bucket u (all documents); nothing is summed in an order that changes from run to run.
  * A call whose total_q is at most 4 x batch is taken as a step of autoregressive decoding (few rows a document, keys

@@ -21,6 +21,7 @@ template <bool BF16, int N> struct Raw;
 template <int N> struct Raw<true, N> {
     uint4 u;
     __device__ __forceinline__ void load(const void *p, unsigned r, int g) { u = __ldg(reinterpret_cast<const uint4 *>(p) + r * N + g); }
+    __device__ __forceinline__ void clear() { u = make_uint4(0, 0, 0, 0); }
     static __device__ __forceinline__ f2 two(uint32_t x) { return pack2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
     __device__ __forceinline__ void get(f2 (&v)[4]) const { v[0] = two(u.x); v[1] = two(u.y); v[2] = two(u.z); v[3] = two(u.w); }
     static __device__ __forceinline__ void store(void *p, unsigned r, int g, const f2 (&v)[4]) {
@@ -53,6 +54,7 @@ template <int N> struct Raw<false, N> {
         const float4 *q = reinterpret_cast<const float4 *>(p) + (size_t)r * (2 * N) + g;
         a = __ldg(q); b = __ldg(q + N);
     }
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load_smem(const float4 *row, int g) { a = row[g]; b = row[N + g]; }
     __device__ __forceinline__ void get(f2 (&v)[4]) const { v[0] = pack2(a.x, a.y); v[1] = pack2(a.z, a.w); v[2] = pack2(b.x, b.y); v[3] = pack2(b.z, b.w); }
     static __device__ __forceinline__ void store(void *p, unsigned r, int g, const f2 (&v)[4]) {

@@ -10,6 +10,8 @@
 // k_self_join (8 documents of 4096 keys, 12 x 64 bf16: 19 us with both launches, 5.3 TB/s; four rows each 43).  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
 #include <math.h>
 
+#include <type_traits>
+
 #include "hdt_rows.cuh"
 #include "hdt_self.cuh"
 
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
         q[r].load((const char *)a.q + ((size_t)(d.q0 + r0 + min(r, nr - 1)) * a.H + h) * ROW, 0u, l);
         S[r].clear();
     }
-    for (int k0 = kb; k0 < ke; k0 += KPI * C) {
+    auto chunk = [&](int k0, auto cut) {      // cut: the first row does not see all of these keys
         if constexpr (AHEAD) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -317,7 +319,12 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
         } else request(k0, x, y);
         const int key = k0 + slot * C + (l & (C - 1));                  // the key whose score this lane keeps
 #pragma unroll
-        for (int r = 0; r < RG; ++r) {
+        for (int i = 0; i < RG; ++i) {
+            const int r = decltype(cut)::value ? RG - 1 - i : i;
+            if constexpr (decltype(cut)::value)      // last row first: the values that a row does not see are taken out for it and those before it (0 times what is not finite is no number)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (k0 + slot * C + c > pos0 + r) y[c].clear();
             float sc[C];
             dots<C>(q[r], x, sc);
             float s = reduce_scatter<C, LPK>(sc, l, mask) * a.scale_log2;
@@ -327,7 +334,13 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
             const float p = S[r].template add<C>(s, mask);
             axpys<C>(S[r].acc, p, y, mask, src);
         }
-    }
+    };
+    // (the last keys apart: the loop over the others has nothing to look at.  In one loop: four rows each of 8 x 4096 keys 33 -> 38 us)
+    const int end = RG > 1 && a.rel.causal ? min(ke, pos0 + 2 - KPI * C) : ke;
+    int k0 = kb;
+    for (; k0 < end; k0 += KPI * C) chunk(k0, std::false_type{});
+    if constexpr (RG > 1)
+        for (; k0 < ke; k0 += KPI * C) chunk(k0, std::true_type{});
 #pragma unroll
     for (int r = 0; r < RG; ++r) {
         if (r > 0 && r >= nr) break;

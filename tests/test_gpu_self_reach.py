@@ -1,4 +1,4 @@
-"""What a row that is not finite reaches in the fp32 kernels: the rows that see it, and no other.
+"""What a row that is not finite reaches in the fp32 kernels and in a step of decoding: the rows that see it, and no other.
 The rest of a call's results are compared with those of the same call on finite rows, bit by bit."""
 import pytest
 import torch
@@ -64,4 +64,25 @@ def test_query_row_reaches_the_keys_that_it_sees(d, bad, with_bias, n, nk, at):
         dq1, dk1, dv1, _ = P.hdt_self_attn_bwd(*a, q1, k, v, o2, lse2, do1, bias=bias)
         assert torch.equal(dk1[last + 1:], dk[last + 1:]) and torch.equal(dv1[last + 1:], dv[last + 1:])
         assert torch.equal(dq1[others], dq[others])
+    P.hdt_device_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("keys", [4, 37, 900])
+def test_step_of_several_rows(dtype, d, bad, keys):
+    """Four and three rows of two documents: the last keys are seen by the last rows only."""
+    import paper_2407_08330_b200 as P
+    q, k, v, _, bias = tensors(7, keys + 50, 3, d, dtype, seed=2)
+    a = (cu(0, 4, 7), cu(0, keys, keys + 50))
+    o, lse = P.hdt_self_attn_fwd(*a, q, k, v, bias=bias)
+    for back in range(3):           # the key that only the last `back` + 1 rows see
+        k1, v1 = k.clone(), v.clone()
+        for end in (keys, keys + 50):
+            k1[end - 1 - back] = v1[end - 1 - back] = bad
+        o1, lse1 = P.hdt_self_attn_fwd(*a, q, k1, v1, bias=bias)
+        clean = list(range(0, 3 - back)) + list(range(4, 6 - back))
+        assert torch.equal(o1[clean], o[clean]) and torch.equal(lse1[:, clean], lse[:, clean])
+        assert not o1[[i for i in range(7) if i not in clean]].isfinite().any()
     P.hdt_device_status()
