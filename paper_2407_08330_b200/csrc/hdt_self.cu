@@ -50,13 +50,18 @@ __device__ __forceinline__ float bias_base2(const void *table, size_t i, int dty
     return (isfinite(v) ? fminf(fmaxf(v, -SELF_MAX_BIAS), SELF_MAX_BIAS) : v) * 1.4426950408889634f;
 }
 
-// Inclusive scan over the CTA's 1024 threads.
+// x + y of numbers that are not negative, at most the largest of them: documents that overlap may have any number of blocks.
+__host__ __device__ __forceinline__ int add_up_to_most(int x, int y) {
+    const unsigned v = (unsigned)x + (unsigned)y;
+    return v > 0x7fffffffu ? 0x7fffffff : (int)v;
+}
+// Inclusive scan over the CTA's 1024 threads, of such sums.
 __device__ __forceinline__ int scan1024(int v, int *s_warp) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += y;
+        if (lane >= o) v = add_up_to_most(v, y);
     }
     if (lane == 31) s_warp[warp] = v;
     __syncthreads();
@@ -65,12 +70,12 @@ __device__ __forceinline__ int scan1024(int v, int *s_warp) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, w, o);
-            if (lane >= o) w += y;
+            if (lane >= o) w = add_up_to_most(w, y);
         }
         s_warp[lane] = w;
     }
     __syncthreads();
-    v += warp > 0 ? s_warp[warp - 1] : 0;
+    if (warp > 0) v = add_up_to_most(v, s_warp[warp - 1]);
     __syncthreads();
     return v;
 }
@@ -128,10 +133,9 @@ __global__ void __launch_bounds__(1024) k_self_prep(const __grid_constant__ Prep
             } else L.raw[x.id] = x;
             atomicAdd(&s_bin[BINS - 1 - min(x.tiles, BINS - 1)], 1);
         }
-        total += n;
+        total = min(add_up_to_most(total, n), L.most);      // (so that the next documents' numbers stay inside 32 bits)
         __syncthreads();
     }
-    total = min(total, L.most);
     const int n_bin = s_bin[t];
     const int start = scan1024(n_bin, s_warp) - n_bin;      // (its barriers lie between the last read and the next write)
     s_bin[t] = start;
@@ -199,10 +203,10 @@ __global__ void __launch_bounds__(1024) k_self_items(const __grid_constant__ Ste
             several |= cut.pieces > 1;
         }
         const int pre = scan1024(n, s_warp);
-        if (b < a.B) a.before[b] = base + pre - n;
+        if (b < a.B) a.before[b] = add_up_to_most(base, pre - n);
         if (threadIdx.x == 1023) s_sum = pre;
         __syncthreads();
-        base += s_sum;
+        base = add_up_to_most(base, s_sum);
         __syncthreads();
     }
     several = __syncthreads_or(several);
