@@ -566,7 +566,8 @@ int sizes_check(int B, int Tq, int Tk, int H, int D, int buckets, int max_distan
     if (D != 64 && D != 128) return set_error(HDT_ERR_UNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
     if (dtype != HDT_F32 && dtype != HDT_BF16) return set_error(HDT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (H > 65535 || (long long)(Tq > Tk ? Tq : Tk) + B > 0x7ffff000LL) return set_error(HDT_ERR_UNSUPPORTED, "%s: more rows or heads than the kernels' grids hold", who);
-    if (blocks(Tq > Tk ? Tq : Tk, B, SELF_F32_ROWS) * H > 0x7ffff000LL || step_items(B, Tq, Tk, H, step_group(B, Tq)) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fff0000LL))
+    // (documents that overlap may fill the lists of both sides, and the fp32 kernels walk both with a stride of up to 2^20)
+    if ((blocks(Tq, B, SELF_F32_ROWS) + blocks(Tk, B, SELF_F32_ROWS)) * H > 0x7fe00000LL || step_items(B, Tq, Tk, H, step_group(B, Tq)) * H > 0x7ffff000LL || (is_step(B, Tq) && (long long)Tq * H > 0x7fff0000LL))
         return set_error(HDT_ERR_UNSUPPORTED, "%s: more blocks than the kernels' grids hold", who);
     if (buckets > 0) {
         const int one = causal ? buckets : buckets / 2;

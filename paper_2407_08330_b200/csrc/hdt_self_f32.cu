@@ -15,7 +15,7 @@
 namespace hdt {
 namespace {
 
-constexpr long long MOST_CTAS = 1 << 20;          // (a CTA walks units with the grid's stride beyond that)
+constexpr long long MOST_CTAS = 1 << 20;          // (a CTA walks units with the grid's stride beyond that; the host's limits of sizes leave room for one in 32 bits)
 constexpr int R = SELF_F32_ROWS, PS = R + 4;      // row stride of a transposed 64 x 64 matrix
 template <int D>
 struct Shape { static constexpr int XS = D + 4, X = R * XS; };
