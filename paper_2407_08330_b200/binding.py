@@ -366,6 +366,16 @@ def hdt_cross_attn_bwd(level, cu_seqlens_k, cu_seqlens_q, level_mask, q, k, v, o
     return dq, dk, dv
 
 
+def _fit(*sizes):
+    """The C interface's sizes have 32 bits (ctypes takes others modulo 2^32)."""
+    return max(sizes) < 2 ** 31 and min(sizes) >= -2 ** 31
+
+
+def _sizes(*sizes):
+    if not _fit(*sizes):
+        raise HdtError(-3, f"sizes must fit 32 bits: {sizes}")
+
+
 def _here(*tensors):
     """The tensors of a call are contiguous and on the current device, whose current stream the call goes to."""
     dev = torch._C._cuda_getDevice()
@@ -397,6 +407,8 @@ def _rows(x):
     """(rows, columns, type): all dimensions but the last are rows."""
     if x.dim() < 1 or x.dtype not in _DTYPES:
         raise HdtError(-3, "rows must be float32 or bfloat16")
+    if x.shape[-1] >= 2 ** 31:
+        raise HdtError(-3, "sizes must fit 32 bits")
     return (x.numel() // x.shape[-1] if x.shape[-1] else 0), x.shape[-1], _DTYPES[x.dtype]
 
 
@@ -447,7 +459,7 @@ def hdt_layer_norm_fwd(x, weight, bias, eps=1e-5, residual=None, p=0.0, rng=None
 
 @functools.lru_cache(maxsize=256)
 def hdt_layer_norm_workspace_bytes(rows, cols) -> int:
-    return int(lib().hdt_layer_norm_workspace_bytes(rows, cols))
+    return 0 if not _fit(cols, 0) else int(lib().hdt_layer_norm_workspace_bytes(rows, cols))
 
 
 def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, site=0, d_residual=None, d_x=None, d_weight=None, d_bias=None,
@@ -477,17 +489,20 @@ def hdt_layer_norm_bwd(d_y, h, mean, rstd, weight, d_h=None, p=0.0, rng=None, si
 
 @functools.lru_cache(maxsize=256)
 def hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, causal, dtype, bwd) -> int:
+    if not _fit(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance):
+        return 0
     return int(lib().hdt_self_workspace_bytes(batch, total_q, total_k, heads, head_dim, num_buckets, max_distance, int(causal), _DTYPES[dtype], int(bwd)))
 
 
 def hdt_self_bucket_borders(num_buckets, max_distance, causal=True):
     """Smallest distance of every bucket of one direction (a list of num_buckets, or of half of them if not causal)."""
+    _sizes(num_buckets, max_distance)
     first = (C.c_int32 * max(1, num_buckets))()
     _check(lib().hdt_self_bucket_borders(int(num_buckets), int(max_distance), int(bool(causal)), first))
     return list(first)[:num_buckets if causal else num_buckets // 2]
 
 
-def _self_common(cu_q, cu_k, seqlens_k, q, k, v, bias):
+def _self_common(cu_q, cu_k, seqlens_k, q, k, v, bias, max_distance):
     if q.dim() != 3 or q.dtype not in _DTYPES or k.shape[1:] != q.shape[1:] or k.dtype != q.dtype:
         raise HdtError(-1, "q, k and v must be [rows, heads, head_dim], float32 or bfloat16 alike")
     _like(k, v)
@@ -497,7 +512,9 @@ def _self_common(cu_q, cu_k, seqlens_k, q, k, v, bias):
             raise HdtError(-1, "offsets must be int32 [batch + 1], lengths int32 [batch]")
     if bias is not None and (bias.dim() != 2 or bias.shape[1] != q.shape[1] or bias.dtype != q.dtype):
         raise HdtError(-1, "bias must be [num_buckets, heads] of q's type")
-    return B, q.shape[0], k.shape[0], q.shape[1], q.shape[2], (0 if bias is None else bias.shape[0])
+    sizes = B, q.shape[0], k.shape[0], q.shape[1], q.shape[2], (0 if bias is None else bias.shape[0])
+    _sizes(*sizes, max_distance)
+    return sizes
 
 
 def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distance=128, causal=True, softmax_scale=0.0, seqlens_k=None, out=None,
@@ -505,7 +522,7 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
     """Self-attention of packed documents with a bias [num_buckets, heads] by relative position: q [Tq,H,d] (the last rows
     of every document), k, v [Tk,H,d]; seqlens_k [batch] where a document's part of k and v has room behind its keys (a
     cache).  Returns (O [Tq,H,d], LSE [H,Tq])."""
-    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
+    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, max_distance)
     _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, out, lse, workspace)
     _like(q, out)
     if lse is not None and (lse.shape != (H, Tq) or lse.dtype != torch.float32):
@@ -525,7 +542,7 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
 def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=None, max_distance=128, causal=True, softmax_scale=0.0, seqlens_k=None,
                       dq=None, dk=None, dv=None, d_bias=None, workspace=None):
     """Gradients (dQ, dK, dV, dBias) of hdt_self_attn_fwd; dBias is None without a bias."""
-    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias)
+    B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, max_distance)
     _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, o, lse, d_o, dq, dk, dv, d_bias, workspace)
     _like(q, o, d_o, dq)
     _like(k, dk, dv)
