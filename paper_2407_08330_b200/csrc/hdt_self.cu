@@ -685,12 +685,14 @@ extern "C" int hdt_self_attn_fwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         if (head_dim == 64) return dtype == HDT_BF16 ? step_rows<64, true>(s, st) : step_rows<64, false>(s, st);
         return dtype == HDT_BF16 ? step_rows<128, true>(s, st) : step_rows<128, false>(s, st);
     }
+    int *const status = device_status_ptr();
+    if (!status) return HDT_ERR_CUDA;
     Prepared p;
     if (const int rc = prepare(L, ws, cu_seqlens_q, cu_seqlens_k, seqlens_k, batch, total_q, total_k, heads, num_buckets, max_distance, causal, bias, dtype, 0, st, &p)) return rc;
     SelfFwdArgs a{};
     a.q = p.q; a.block_rows = L.rows_q; a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0;
     a.qp = q; a.kp = k; a.vp = v; a.o = o; a.lse = lse; a.scale_log2 = scale * LOG2E;
-    a.status = device_status_ptr();
+    a.status = status;
     return dtype == HDT_BF16 ? launch_self_fwd_tc(a, head_dim, st) : launch_self_fwd_f32(a, head_dim, st);
 }
 
@@ -718,6 +720,8 @@ extern "C" int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         for (const void *x : {q, k, v, o, d_o, (const void *)dq, (const void *)dk, (const void *)dv})
             if (const int rc = ptr_check(x, who)) return rc;
         if (!lse || ((uintptr_t)lse & 3)) return set_error(HDT_ERR_INVALID_ARG, "%s: null or misaligned tensor", who);
+        int *const status = device_status_ptr();
+        if (!status) return HDT_ERR_CUDA;
         // (delta first: the preparation runs beside it)
         if (const int rc = launch_delta(o, d_o, (float *)(ws + L.delta), total_q, heads, head_dim, dtype, st)) return rc;
         if (const int rc = prepare(L, ws, cu_seqlens_q, cu_seqlens_k, seqlens_k, batch, total_q, total_k, heads, num_buckets, max_distance, causal, bias, dtype, 1, st, &p)) return rc;
@@ -725,7 +729,7 @@ extern "C" int hdt_self_attn_bwd(const int32_t *cu_seqlens_q, const int32_t *cu_
         SelfBwdArgs a{};
         a.dist = p.dist; a.H = heads; a.Tq = total_q; a.Tk = total_k; a.causal = causal; a.bias_on = num_buckets > 0; a.buckets = num_buckets;
         a.qp = q; a.kp = k; a.vp = v; a.dop = d_o; a.lse = lse; a.delta = (float *)(ws + L.delta); a.dq = dq; a.dk = dk; a.dv = dv;
-        a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.status = device_status_ptr();
+        a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.status = status;
         SelfBwdArgs keys = a, rows = a;
         keys.blk = p.k;
         rows.blk = p.q;
