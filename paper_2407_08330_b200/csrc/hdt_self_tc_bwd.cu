@@ -67,12 +67,12 @@ __device__ __forceinline__ bool group_all(bool pred, int id, int n) {      // ba
 
 template <int D, bool ROWS>
 struct BwdShape {
-    static constexpr int NS = D / 64, TILE = SUB * NS, RES = 1, ST = D == 64 ? 4 : 2;
+    static constexpr int NS = D / 64, TILE = SUB * NS, ST = D == 64 ? 4 : 2;
     static constexpr bool RTM = D == 64;                      // the resident tiles are read from TMEM
     static constexpr uint32_t TM_S = 0, TM_P = 128, TM_ACC = 256, TM_R = 384;
     static constexpr int STAT = 128 * 8 + 256 * 4 + 256;      // -LSE', -delta' by column; bias' and bucket by distance
     static constexpr int SUMS = ROWS ? 4 * 128 * 4 : 16 * (SELF_MAX_BUCKETS + 32) * 4;
-    static constexpr int SMEM = (RES * 2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
+    static constexpr int SMEM = (2 + ST * 2) * TILE + SUB + ST * STAT + SUMS + 512;
 };
 }  // namespace
 
@@ -139,13 +139,13 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                                                      const __grid_constant__ CUtensorMap tm_s1, const __grid_constant__ CUtensorMap tm_s2,
                                                      const __grid_constant__ StoreMaps sm_out, const SelfBwdArgs a) {
     using Sh = BwdShape<D, ROWS>;
-    constexpr int NS = Sh::NS, TILE = Sh::TILE, RES = Sh::RES, ST = Sh::ST;
+    constexpr int NS = Sh::NS, TILE = Sh::TILE, ST = Sh::ST;
     constexpr uint32_t TM_S = Sh::TM_S, TM_P = Sh::TM_P, TM_ACC = Sh::TM_ACC, TM_R = Sh::TM_R, TM_COLS = 512;
     constexpr bool RTM = Sh::RTM;
     constexpr int W_DRAIN = 16, W_LOAD = 20, W_MMA = 21;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    uint8_t *sR = smem_raw;                       // [RES] x {R1, R2}: K, V or Q, dO
-    uint8_t *sS = sR + RES * 2 * TILE;            // [ST] x {S1, S2}: Q, dO or K, V
+    uint8_t *sR = smem_raw;                       // R1, R2: K, V or Q, dO
+    uint8_t *sS = sR + 2 * TILE;                  // [ST] x {S1, S2}: Q, dO or K, V
     uint8_t *sStg = sS + ST * 2 * TILE;           // staging of 64 columns of a result
     uint8_t *sStat = sStg + SUB;                  // [ST] x STAT
     float *sSum = (float *)(sStat + ST * Sh::STAT);        // rows: [4][128] row sums of dS; keys: per compute warp [buckets] and [32] of scratch
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             const int x = warp >> 3, qh = (warp >> 2) & 1, rl = (warp & 3) * 32 + lane, c0 = 64 * x + 32 * qh;
             float *sum = sSum + warp * (SELF_MAX_BUCKETS + 32), *scratch = sum + SELF_MAX_BUCKETS;      // (keys)
             const uint32_t tm_s = tmem + TM_S + 64u * x + 32u * qh + lane_base, tm_dp = tmem + TM_P + 64u * x + 32u * qh + lane_base;
-            int st = 0, tp = 0, uc = 0, par = 0;
+            int st = 0, uc = 0, par = 0;
             auto flush = [&](float v, int at) {      // a warp's sum beyond the borders, to the bucket of distance number `at`
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&ds_ready[x]);
-                    if (++st == ST) { st = 0; tp ^= 1; }
+                    if (++st == ST) st = 0;
                     par ^= 1;
                     if (!HDT_AGREE()) break;
                     if (!(sums && near && any)) continue;
@@ -428,17 +428,15 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
             for (int k = 0, u; ok && (u = self_unit(k, blockIdx.x, gridDim.x)) < n_units; ++k) {
                 const Unit x = unit(u);
                 if (x.nt == 0) continue;
-                const int rb = uc % RES, rround = uc / RES;
-                if (rround > 0) HDT_WAIT(&r_empty[rb], (rround - 1) & 1, 1);
+                if (uc > 0) HDT_WAIT(r_empty, (uc - 1) & 1, 1);
                 if (!HDT_AGREE()) break;
                 if (lane == 0) {
                     const int row = (ROWS ? x.b.q0 : x.b.k0) + x.b.r0;
-                    uint8_t *d = sR + rb * 2 * TILE;
-                    mbar_expect_tx(&r_full[rb], 2u * TILE);
+                    mbar_expect_tx(r_full, 2u * TILE);
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        tma_load_3d(d + s * SUB, &tm_r1, 64 * s, x.h, row, &r_full[rb]);
-                        tma_load_3d(d + TILE + s * SUB, &tm_r2, 64 * s, x.h, row, &r_full[rb]);
+                        tma_load_3d(sR + s * SUB, &tm_r1, 64 * s, x.h, row, r_full);
+                        tma_load_3d(sR + TILE + s * SUB, &tm_r2, 64 * s, x.h, row, r_full);
                     }
                 }
                 ++uc;
@@ -629,8 +627,7 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                 while ((u = self_unit(k_move, blockIdx.x, gridDim.x)) < n_units && unit(u).nt == 0) ++k_move;
                 if (u >= n_units) return;
                 ++k_move;
-                const uint8_t *r = sR + (um % RES) * 2 * TILE;
-                HDT_WAIT(&r_full[um % RES], (um / RES) & 1, 16);
+                HDT_WAIT(r_full, um & 1, 16);
                 if (um > 1) HDT_WAIT(&r_free[um & 1], ((um >> 1) - 1) & 1, 17);
                 if (!HDT_AGREE()) return;
                 tc_fence_after();
@@ -639,14 +636,14 @@ __global__ void __launch_bounds__(768, 1) k_self_bwd(const __grid_constant__ CUt
                     uint32_t y[16];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint4 z = *reinterpret_cast<const uint4 *>(r + (q >> 1) * TILE + swz(rl, 4 * (q & 1) + e));
+                        const uint4 z = *reinterpret_cast<const uint4 *>(sR + (q >> 1) * TILE + swz(rl, 4 * (q & 1) + e));
                         y[4 * e] = z.x; y[4 * e + 1] = z.y; y[4 * e + 2] = z.z; y[4 * e + 3] = z.w;
                     }
                     tmem_st16(tmem + TM_R + 64u * (um & 1) + 16u * q + lane_base, y);
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(&r_empty[um % RES]);
+                mbar_arrive(r_empty);
                 mbar_arrive(&r_ready[um & 1]);
                 ++um;
             };
