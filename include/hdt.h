@@ -313,7 +313,7 @@ int hdt_cross_attn_bwd(const int8_t *level, const int32_t *cu_seqlens_k, const i
  *   Eight columns of a row take one 128-bit block of Philox-4x32-10 (Salmon et al., SC 2011): key = the 64 bits of
  *   seed, counter = (column / 8, row, site, low 32 bits of offset).  Column c keeps its value if the (c mod 8)-th
  *   16-bit half word of the block (low half of a word first) is at least t = floor(65536 p + 1/2), t <= 65535, and is
- *   then multiplied by 65536 / (65536 - t).
+ *   then multiplied by 65536 / (65536 - t).  A value that is dropped counts as 0 even where it is not finite.
  *   x, residual, y     device [rows, cols] of `dtype`, contiguous; residual may be NULL; y may be x or residual
  *   rng                device int64 [2]: seed, offset.  In device memory, so that a captured graph draws a new mask
  *                      at every replay once its caller has advanced the offset
@@ -380,6 +380,8 @@ int hdt_layer_norm_bwd(const void *d_y, const void *d_h, const void *h, const fl
  * the gradients.  Offsets outside [0, total] are clamped; documents that overlap are not written whole.  bf16: a row of a document
  * that is not finite reaches the document's other rows of its tile; fp32, and a step of decoding (below): the rows that
  * see it, and no other.  Other documents never do.
+ * bf16: sums, softmax statistics, accumulators and d_bias are fp32; P and dS are rounded to bf16 for their products with V, K, Q and
+ * d_o (a step of decoding keeps P in fp32), which in O and the gradients is another error of about the size of their own rounding.
  * Backward: dS = P o (d_o V^T - delta), dQ = scale dS K, dK = scale dS^T Q, dV = P^T d_o, d_bias[u][h] = sum of dS over the
  * pairs of bucket u (all documents); nothing is summed in an order that changes from run to run.
  * A call whose total_q is at most 4 x batch is taken as a step of autoregressive decoding (few rows a document, keys

@@ -521,7 +521,8 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
                       lse=None, workspace=None):
     """Self-attention of packed documents with a bias [num_buckets, heads] by relative position: q [Tq,H,d] (the last rows
     of every document), k, v [Tk,H,d]; seqlens_k [batch] where a document's part of k and v has room behind its keys (a
-    cache).  Returns (O [Tq,H,d], LSE [H,Tq])."""
+    cache).  Returns (O [Tq,H,d], LSE [H,Tq]).  Rows of no document are not written: where there are such rows, give `out` and `lse`
+    what they are to hold."""
     B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, max_distance)
     _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, out, lse, workspace)
     _like(q, out)
@@ -541,7 +542,8 @@ def hdt_self_attn_fwd(cu_seqlens_q, cu_seqlens_k, q, k, v, bias=None, max_distan
 
 def hdt_self_attn_bwd(cu_seqlens_q, cu_seqlens_k, q, k, v, o, lse, d_o, bias=None, max_distance=128, causal=True, softmax_scale=0.0, seqlens_k=None,
                       dq=None, dk=None, dv=None, d_bias=None, workspace=None):
-    """Gradients (dQ, dK, dV, dBias) of hdt_self_attn_fwd; dBias is None without a bias."""
+    """Gradients (dQ, dK, dV, dBias) of hdt_self_attn_fwd; dBias is None without a bias.  Rows of no document (and keys behind seqlens_k)
+    are not written: where there are such rows, give dq, dk and dv zeros."""
     B, Tq, Tk, H, d, n = _self_common(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, max_distance)
     _here(cu_seqlens_q, cu_seqlens_k, seqlens_k, q, k, v, bias, o, lse, d_o, dq, dk, dv, d_bias, workspace)
     _like(q, o, d_o, dq)

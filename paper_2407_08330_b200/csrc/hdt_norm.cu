@@ -17,7 +17,9 @@
 // fixed order too: no atomics, the same bits every run.
 //
 // Measured, bf16: dropout and residual on 65536 x 1024 61 us, 6.6 TB/s; forward with both on 32768 x 768 37 us, 5.5 TB/s; its
-// backward with dH 53 us, 4.8 TB/s, and 6 us for the last sum of the columns.
+// backward with dH 53 us, 4.8 TB/s, and 6 us for the last sum of the columns.  The backward is held up by HBM's latency and not by its
+// rate: 168 registers a thread leave twelve warps to an SM, each with one row of dY and h in flight (without dropout and dH
+// 32768 x 768 36 us, 4.2 TB/s, 16384 x 2048 65 us, 3.1; issue slots 49 and 35 %, loads the longest stall).
 #include "hdt_internal.cuh"
 #include "hdt_philox.cuh"
 

@@ -135,7 +135,7 @@ __device__ __forceinline__ void store8(T *row, int chunk, int l, int cols, const
         }
     }
 }
-// The lane's eight columns of a chunk times their keep mask.  All lanes of the warp call it.
+// The lane's eight columns of a chunk times their keep mask; what is dropped is 0 whatever it was.  All lanes of the warp call it.
 template <int LPR, bool VEC>
 __device__ __forceinline__ void drop8(const PhiloxKey &k, const Drop &d, uint32_t row, int chunk, int l, float (&v)[8]) {
     const uint4 x = philox(k, (uint32_t)(chunk * LPR + l), row, d.site);

@@ -7,7 +7,8 @@
 //
 // Decoding (few rows per document): bound by HBM, the keys and values once.  A warp takes a piece of a document's keys for
 // one head and up to four rows; every lane group has a softmax of its own, joined at the piece's end, the pieces by
-// k_self_join (8 documents of 4096 keys, 12 x 64 bf16: 19 us with both launches, 5.3 TB/s; four rows each 43).  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
+// k_self_join (8 documents of 4096 keys, 12 x 64, caches that L2 does not hold, with both launches: bf16 23 us, 4.4 TB/s, fp32 36, 5.6; four
+// rows each 45 and 52; a cache of bf16 that L2 holds for the most part 18).  A document with more rows takes longer pieces, so that the number of pieces is bounded by the keys.
 #include <math.h>
 
 #include <type_traits>
@@ -233,8 +234,9 @@ __device__ __forceinline__ int last_at_most(int n, int x, F get) {
     return -1;
 }
 // The document that item x, or row x, lies in, and how many items come before the document (whole warp).  Up to 64 documents, whose
-// loads are two rounds, every warp counts; beyond, k_self_items has, and the document is searched for (65 documents: 21.5 us
-// counted, 22.3 searched; 128: 48.9 and 48.1; 1000: 268 and 82; 4000: 3138 and 220; pieces since then other ones).
+// loads are two rounds, every warp counts; beyond, k_self_items has, and the document is searched for.  12 x 64 bf16, counted and
+// searched: 32 x 100 keys 9.8 and 12.1 us, 64 x 500 23.0 and 25.6, 65 x 500 23.9 and 25.2, 128 x 100 18.2 and 16.2, 128 x 500 44.7 and
+// 42.8, 1000 x 100 330 and 73, 4000 x 50 4014 and 180.
 template <int RG, bool BY_ROW>
 __device__ __forceinline__ bool find_doc(const StepArgs &a, int x, Doc &d, int &before) {
     if (a.before != nullptr) {
@@ -339,7 +341,7 @@ __global__ void __launch_bounds__(128, RG == 1 ? 4 : 3) k_self_step(const __grid
             axpys<C>(S[r].acc, p, y, mask, src);
         }
     };
-    // (the last keys apart: the loop over the others has nothing to look at.  In one loop: four rows each of 8 x 4096 keys 33 -> 38 us)
+    // (the last keys apart: the loop over the others has nothing to look at.  In one loop: four rows each of 8 caches of 1024 to 4096 keys 33 -> 38 us)
     const int end = RG > 1 && a.rel.causal ? min(ke, pos0 + 2 - KPI * C) : ke;
     int k0 = kb;
     for (; k0 < end; k0 += KPI * C) chunk(k0, std::false_type{});
@@ -504,8 +506,9 @@ constexpr int STEP_ROWS = 4;      // rows per document, on average, up to which 
 bool is_step(int B, int Tq) { return B > 0 && Tq <= STEP_ROWS * (long long)B; }
 // Keys of a piece, for documents of one length (the host knows no other): a piece is a warp, `most` of them are resident at once and
 // take turns in waves, and a warp takes about as long to begin as for 32 keys.  Of the pieces that fill 1 .. 8 waves, those that
-// are done first.  (Against one wave of fourteen warps to an SM: 8 x 4096 keys 19.4 -> 18.0 us, 128 x 500 48 -> 42, 100 x 3000 209 -> 155;
-// at most 256 keys: 100 x 3000 157, but 64 x 2000 72 -> 66 here, 128 x 500 50.)
+// are done first.  (Against one wave of fourteen warps to an SM: 8 x 4096 keys, which L2 held for the most part, 19.4 -> 18.0 us, 128 x 500
+// 48 -> 42, 100 x 3000 209 -> 155; at most 256 keys: 100 x 3000 157, but 64 x 2000 72 -> 66 here, 128 x 500 50.)  The documents' room is
+// what the host knows: where a third of a cache is unused, a third of the warps has nothing to do.
 int step_piece(int B, int Tk, int H, int rg) {
     const long long most = (rg == 1 ? 16 : 12) * PLAN_SMS, b = B > 0 ? B : 1, keys = (Tk + b - 1) / b;
     long long best = 0, piece = 64;

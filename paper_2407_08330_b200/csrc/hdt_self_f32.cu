@@ -4,7 +4,7 @@
 // reads of neighbouring threads lie in different banks) and 4 rows x D / 16 columns of a result (rows 4 ty + i, columns
 // 4 tx + 64 j).  A 64 x 64 product matrix goes from the one layout to the other through shared memory, transposed.
 // Bound by the shared-memory reads (two of 16 bytes for 16 fma) and, in short calls, by the longest document's last block: 2 x 777
-// tokens, 12 x 64, forward 99 us and backward 271, 19 and 17 TFLOP/s.  Rows behind a document's end are stored as zeros.
+// tokens, 12 x 64, forward 98 us and backward 270, 19 and 17 TFLOP/s.  Rows behind a document's end are stored as zeros.
 //
 // Forward: running maximum and sum of the softmax, O rescaled at every tile.  Backward as in bf16: once with keys resident
 // (dK, dV), once with rows resident (dQ, and the bias' gradient: the sums along the diagonals of the tile's dS, then by

@@ -14,9 +14,11 @@
 // a tile's exceeds it by more than 8 (a factor of 256 that fp32 sums and bf16 P both have room for), so O is rescaled on few
 // tiles.  P is rounded to bf16 for the product (8 significant bits, relative, as V has); the row sum adds it unrounded.
 //
-// Bound by the exponentials' unit and the way from S to P: at head_dim 64 a pair of tiles needs 1024 cycles of products, 2048 of
-// exponentials, and takes 3660 (1 x 16384 tokens, 12 heads, both ways 1237 us, 667 TFLOP/s; causal 4 x 4096 182 us, 567 of
-// unmasked pairs, and with 16 heads of 128 278 us, 989).
+// At head_dim 64 a pair of tiles needs 1024 cycles of products, 2048 of exponentials, and takes 3660 (1 x 16384 tokens, 12 heads, both
+// ways 1237 us, 667 TFLOP/s; causal 4 x 4096 182 us, 567 of unmasked pairs, and with 16 heads of 128 278 us, 989).  No unit is full there:
+// exponentials 67 % of the time on the SMs with the most units (768 units on 148 SMs: six at most, 5.2 on average), tensor pipe 34 %
+// and issue slots 38 % of active cycles.  What takes the time is a tile's chain (S, maximum, exponentials, P stored and fenced as a
+// whole, product), which two row tiles cover in part; an SM's TMEM has no room for a third.
 //
 // The rows of V behind a document's last key are set to zero in shared memory: P is 0 there, but another document's rows,
 // or a cache's unused ones, may hold NaN.
